@@ -358,6 +358,59 @@ int svdq_linear_mxfp4_next(const uint8_t* qx, const uint8_t* sx_e8m0, const void
                            uint8_t* next_qx, uint8_t* next_sx_e8m0, float* next_h, void* stream);
 
 /*
+ * ---- The layer in 8 bits, for the modules that a 4-bit model keeps at more bits (attention output and feed-forward
+ * down-projection, Sec. IV) and for any linear whose weights come as 8-bit codes.  One scale a token and one a channel:
+ *   x^ = x * inv_lambda (eq. 5), a = max_k |x^|, s = (rho*a)/127, q = clip(rne(x^ * (1/s)), -127, 127)     eq. 3, 8, 9
+ *   y[m,n] = (sum_k q[m,k] qw[n,k]) * s[m] * sw[n] + bias[n]
+ * each step of the codes and scales a single IEEE binary32 operation (bit-exact), the sum exact in 32-bit integers, y rounded once
+ * from binary32.  A row of x with a NaN or an infinity (or whose x^ overflows) gets scale NaN and codes 0, so its row of y is NaN
+ * and no other is; a scale that would not be a normal number is 0, with codes 0.  No low-rank branch.
+ * Codes and weights are row-major, one byte a value, as such checkpoints hold them; nothing is packed.
+ *
+ *   svdq_quantize_act_int8   x_bf16 [M, ldx] bf16, ldx >= K, ldx % 8 == 0; inv_lambda [K] binary32 or NULL (ones); rho in (0, 1];
+ *                            gelu != 0: of bf16(gelu(x)), as svdq_quantize_act_gelu defines it;
+ *                            out qx [M, K] int8 and sx [M] binary32
+ *   svdq_linear_w8a8         qx, sx as above (any int8 codes); qw [N, K] int8, sw [N], bias [N] binary32 or NULL;
+ *                            out y [M, ldy] bf16 or binary32, ldy >= N
+ * K % 16 == 0, K <= SVDQ_MAX_K_INT8; any N >= 1 and M.  x, inv_lambda, qx and qw are 16-byte aligned; vectors of scales, ratios and
+ * biases and y are aligned as their elements (y is stored fastest with 16-byte aligned rows).
+ *
+ * Grouped by expert: row i of qx, sx and y belongs to the expert e with offsets[e] <= i < offsets[e + 1], of E experts
+ * (1 <= E <= SVDQ_MAX_EXPERTS) with qw [E, N, K], sw [E, N], bias [E, N] and inv_lambda [E, K].  offsets: E + 1 ascending int32 on the
+ * device, in [0, M]; equal neighbours are experts without rows.  Rows in front of offsets[0] and from offsets[E] on are not written.
+ * Offsets that break this are read as their running maximum, cut to [0, M]: rows may then be another expert's, but no access
+ * leaves the arrays.
+ *   svdq_quantize_act_int8_grouped   row i is made of row rows[i] of x [x_rows, ldx] (rows: M int32 on the device, in any order and any number of
+ *                            times each; a number outside [0, x_rows) counts as a row of zeros), or with rows NULL of row i
+ *                            of x [M, ldx]; row_rho [M] binary32 on the device holds each row's ratio (not checked: one that is not
+ *                            positive gives scale 0, a NaN scale NaN), or NULL for rho
+ *   svdq_linear_w8a8_grouped
+ *   svdq_layer_int8_forward  both halves of a layer in one call, of either form.  E == 0: not grouped (rows, offsets and row_rho NULL).
+ *                            qx [M, K] and sx [M] receive codes and scales.  y bf16; it may share memory with x, and with nothing else.
+ */
+enum { SVDQ_MAX_K_INT8 = 32768, SVDQ_MAX_EXPERTS = 1024 };
+int svdq_quantize_act_int8(const void* x_bf16, int64_t ldx, const float* inv_lambda, float rho, int gelu,
+                           int64_t M, int K, int8_t* qx, float* sx, void* stream);
+int svdq_linear_w8a8(const int8_t* qx, const float* sx, const int8_t* qw, const float* sw, const float* bias,
+                     int64_t M, int N, int K, void* y, int64_t ldy, int out_dtype, void* stream);
+int svdq_quantize_act_int8_grouped(const void* x_bf16, int64_t ldx, int64_t x_rows, const int32_t* rows,
+                                   const int32_t* offsets, int E, const float* inv_lambda, float rho, const float* row_rho, int gelu,
+                                   int64_t M, int K, int8_t* qx, float* sx, void* stream);
+int svdq_linear_w8a8_grouped(const int8_t* qx, const float* sx, const int8_t* qw, const float* sw, const float* bias,
+                             const int32_t* offsets, int E, int64_t M, int N, int K,
+                             void* y, int64_t ldy, int out_dtype, void* stream);
+typedef struct {
+    int E, N, K;
+    const float* inv_lambda;
+    const int8_t* qw;
+    const float* sw;
+    const float* bias;
+} svdq_layer_int8;
+int svdq_layer_int8_forward(const svdq_layer_int8* layer, const void* x_bf16, int64_t ldx, int64_t x_rows, const int32_t* rows,
+                            const int32_t* offsets, float rho, const float* row_rho, int gelu, int64_t M,
+                            int8_t* qx, float* sx, void* y, int64_t ldy, void* stream);
+
+/*
  * Offline calibration, Sec. III-C: the clipping ratio of a (layer, timestep bin) is the candidate that
  * minimises the expected squared reconstruction error || Y - Y^(rho) ||^2 of the quantised layer over
  * the calibration steps of the bin.  The search runs the hot path (svdq_quantize_act* +

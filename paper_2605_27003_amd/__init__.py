@@ -17,4 +17,5 @@ from .binding import (  # noqa: F401
     gptq_hessian, gptq_quantize,
     sq_error, sq_error_static, search_clipping_ratios,
     W4A4Linear,
+    quantize_act_int8, linear_w8a8, quantize_act_int8_grouped, linear_w8a8_grouped, W8A8Linear, W8A8Experts,
 )

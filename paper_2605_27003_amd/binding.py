@@ -54,6 +54,11 @@ EXPORTS = {
     "svdq_sq_error_add": (_i32, [_vp, _i64, _vp, _i64, _i64, _i32, _vp, _vp, _vp]),
     "svdq_argmin_rows": (_i32, [_vp, _i32, _i32, _vp, _vp]),
     "svdq_sq_error_static": (_i32, [_vp, _i64, _vp, _i64, _i64, _i32, _vp, _vp]),
+    "svdq_quantize_act_int8": (_i32, [_vp, _i64, _vp, _f32, _i32, _i64, _i32, _vp, _vp, _vp]),
+    "svdq_linear_w8a8": (_i32, [_vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _vp, _i64, _i32, _vp]),
+    "svdq_quantize_act_int8_grouped": (_i32, [_vp, _i64, _i64, _vp, _vp, _i32, _vp, _f32, _vp, _i32, _i64, _i32, _vp, _vp, _vp]),
+    "svdq_linear_w8a8_grouped": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _i32, _i32, _vp, _i64, _i32, _vp]),
+    "svdq_layer_int8_forward": (_i32, [_vp, _vp, _i64, _i64, _vp, _vp, _f32, _vp, _i32, _i64, _vp, _vp, _vp, _i64, _vp]),
     "svdq_debug_group_acc": (_i32, [_vp, _vp, _i64, _i32, _i32, _i64, _i32, _vp, _vp]),
     "svdq_debug_scale_chain": (_i32, [_vp, _f32, _i64, _vp, _vp, _vp]),
 }
@@ -674,3 +679,215 @@ class W4A4Linear:
             *work.ptrs, None if staging is None else staging.data_ptr(),
             work.y_ptr, self.N, _raw_stream()), "svdq_layer_forward")
         return work.y
+
+
+# ---- the 8-bit layer, and its form grouped by expert ---------------------------------------------
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _need_tensor(name, t, dtype, shape, device):
+    """A contiguous GPU tensor of the type and shape that the kernels read (None in a shape: any size)."""
+    _need(t.dtype == dtype and t.dim() == len(shape) and all(w is None or w == n for w, n in zip(shape, t.shape)) and t.is_contiguous(),
+          f"{name}: a contiguous {dtype} tensor of shape {tuple('any' if n is None else n for n in shape)} is needed, not {t.dtype} {tuple(t.shape)}")
+    _need(t.device == device, f"{name} is on {t.device}, not on {device}")
+
+
+def _need_rows(name, t, dtypes, shape):
+    """A matrix whose rows may be further apart than they are long, on the current GPU; returns its row stride."""
+    _need(t.dim() == 2 and t.dtype in dtypes and all(w is None or w == n for w, n in zip(shape, t.shape)),
+          f"{name}: {' or '.join(map(str, dtypes))} of shape {tuple('any' if n is None else n for n in shape)} is needed, not {t.dtype} {tuple(t.shape)}")
+    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is on {t.device}, not on the current GPU")
+    rows, cols = t.shape
+    _need((cols <= 1 or t.stride(1) == 1) and (rows <= 1 or t.stride(0) >= cols), f"{name}: rows of consecutive values are needed")
+    return t.stride(0) if rows > 1 else max(cols, (cols + 7) & ~7)
+
+
+def _quantize_int8_out(out, M, K, device):
+    if out is None:
+        return torch.empty((M, K), dtype=torch.int8, device=device), torch.empty(M, dtype=torch.float32, device=device)
+    _need_tensor("out[0]", out[0], torch.int8, (M, K), device)
+    _need_tensor("out[1]", out[1], torch.float32, (M,), device)
+    return out
+
+
+def quantize_act_int8(x_bf16, inv_lambda=None, rho=1.0, gelu=False, out=None):
+    """x [M,K] bf16 (row stride allowed) -> (qx [M,K] int8, sx [M] f32): codes of x * inv_lambda (None: of x) with one scale
+    (rho max|.|) / 127 a token; gelu=True: of gelu(x)."""
+    ldx = _need_rows("x", x_bf16, (torch.bfloat16,), (None, None))
+    M, K = x_bf16.shape
+    if inv_lambda is not None:
+        _need_tensor("inv_lambda", inv_lambda, torch.float32, (K,), x_bf16.device)
+    qx, sx = _quantize_int8_out(out, M, K, x_bf16.device)
+    if M == 0:                       # an empty tensor has no address
+        return qx, sx
+    _check(load_library().svdq_quantize_act_int8(_ptr(x_bf16), ldx, _ptr(inv_lambda), float(rho), int(bool(gelu)), M, K,
+                                                 _ptr(qx), _ptr(sx), _stream()), "svdq_quantize_act_int8")
+    return qx, sx
+
+
+def _linear_out(out, M, N, out_dtype, device):
+    """(y, its row stride, its type's code)"""
+    if out is None:
+        _need(out_dtype in (torch.bfloat16, torch.float32), f"out_dtype: bfloat16 or float32, not {out_dtype}")
+        out = torch.empty((M, N), dtype=out_dtype, device=device)
+    else:
+        _need(out.device == device, f"out is on {out.device}, not on {device}")
+        _need_rows("out", out, (torch.bfloat16, torch.float32), (M, N))
+    return out, out.stride(0) if M > 1 else N, OUT_F32 if out.dtype == torch.float32 else OUT_BF16
+
+
+def linear_w8a8(qx, sx, qw, sw, bias=None, out=None, out_dtype=torch.bfloat16):
+    """qx [M,K] int8, sx [M] f32, qw [N,K] int8, sw [N] f32, bias [N] f32 -> y [M,N] = (qx qw^T) sx sw + bias, bf16 or f32."""
+    _need_rows("qx", qx, (torch.int8,), (None, None))
+    (M, K), N, device = qx.shape, qw.shape[0], qx.device
+    _need(qx.is_contiguous(), "qx: a contiguous tensor is needed")
+    _need_tensor("sx", sx, torch.float32, (M,), device)
+    _need_tensor("qw", qw, torch.int8, (None, K), device)
+    _need_tensor("sw", sw, torch.float32, (N,), device)
+    if bias is not None:
+        _need_tensor("bias", bias, torch.float32, (N,), device)
+    y, ldy, code = _linear_out(out, M, N, out_dtype, device)
+    if M == 0:
+        return y
+    _check(load_library().svdq_linear_w8a8(_ptr(qx), _ptr(sx), _ptr(qw), _ptr(sw), _ptr(bias), M, N, K, _ptr(y), ldy, code, _stream()),
+           "svdq_linear_w8a8")
+    return y
+
+
+def _row_rho(rho, M, device):
+    """(the ratio of all rows, or a tensor of every row's)"""
+    if not torch.is_tensor(rho):
+        return float(rho), None
+    _need_tensor("rho", rho, torch.float32, (M,), device)
+    return 1.0, rho
+
+
+def quantize_act_int8_grouped(x_bf16, offsets, inv_lambda=None, rho=1.0, rows=None, gelu=False, out=None):
+    """quantize_act_int8 of rows in the experts' order: expert e owns rows offsets[e] .. offsets[e + 1] (int32 [E + 1]) and smooths them
+    with inv_lambda[e] ([E,K]).  rows (int32 [M], any order, repeats allowed): row i is made of x[rows[i]]; None: of x[i].
+    rho: a number or every row's ratio (f32 [M]).  Rows that no expert owns are not written."""
+    ldx = _need_rows("x", x_bf16, (torch.bfloat16,), (None, None))
+    (x_rows, K), device = x_bf16.shape, x_bf16.device
+    M, E = (x_rows if rows is None else rows.numel()), offsets.numel() - 1
+    _need_tensor("offsets", offsets, torch.int32, (E + 1,), device)
+    if rows is not None:
+        _need_tensor("rows", rows, torch.int32, (M,), device)
+    if inv_lambda is not None:
+        _need_tensor("inv_lambda", inv_lambda, torch.float32, (E, K), device)
+    ratio, row_rho = _row_rho(rho, M, device)
+    qx, sx = _quantize_int8_out(out, M, K, device)
+    if M == 0:
+        return qx, sx
+    _check(load_library().svdq_quantize_act_int8_grouped(
+        _ptr(x_bf16), ldx, x_rows, _ptr(rows), _ptr(offsets), E, _ptr(inv_lambda), ratio, _ptr(row_rho), int(bool(gelu)), M, K,
+        _ptr(qx), _ptr(sx), _stream()), "svdq_quantize_act_int8_grouped")
+    return qx, sx
+
+
+def linear_w8a8_grouped(qx, sx, offsets, qw, sw, bias=None, out=None, out_dtype=torch.bfloat16):
+    """linear_w8a8 grouped by expert: rows offsets[e] .. offsets[e + 1] (int32 [E + 1]) of qx with qw[e] ([E,N,K] int8), sw[e] and bias[e]
+    ([E,N] f32).  Rows that no expert owns are not written."""
+    _need_rows("qx", qx, (torch.int8,), (None, None))
+    _need(qx.is_contiguous(), "qx: a contiguous tensor is needed")
+    _need(qw.dim() == 3, "qw: [E, N, K] is needed")
+    (M, K), (E, N), device = qx.shape, qw.shape[:2], qx.device
+    _need_tensor("sx", sx, torch.float32, (M,), device)
+    _need_tensor("offsets", offsets, torch.int32, (E + 1,), device)
+    _need_tensor("qw", qw, torch.int8, (E, N, K), device)
+    _need_tensor("sw", sw, torch.float32, (E, N), device)
+    if bias is not None:
+        _need_tensor("bias", bias, torch.float32, (E, N), device)
+    y, ldy, code = _linear_out(out, M, N, out_dtype, device)
+    if M == 0:
+        return y
+    _check(load_library().svdq_linear_w8a8_grouped(_ptr(qx), _ptr(sx), _ptr(qw), _ptr(sw), _ptr(bias), _ptr(offsets), E, M, N, K,
+                                                   _ptr(y), ldy, code, _stream()), "svdq_linear_w8a8_grouped")
+    return y
+
+
+class _LayerInt8(ctypes.Structure):
+    """svdq_layer_int8 of include/svdq.h."""
+    _fields_ = [(n, _i32) for n in ("E", "N", "K")] + [(n, _vp) for n in ("inv_lambda", "qw", "sw", "bias")]
+
+
+class _W8A8:
+    """What W8A8Linear and W8A8Experts share.  The tensors are attributes and may be replaced; a call looks at what it finds."""
+
+    def __init__(self, inv_lambda, qw, sw, bias=None):
+        self.inv_lambda, self.qw, self.sw, self.bias = inv_lambda, qw, sw, bias
+        self._held = None
+        self._descriptor()
+
+    def _descriptor(self):
+        """svdq_layer_int8 of the tensors that the layer holds now, checked when they have changed.  The caller keeps it through
+        its call."""
+        tensors = (self.inv_lambda, self.qw, self.sw, self.bias)
+        held = self._held
+        if held is not None and all(a is b for a, b in zip(held[0], tensors)):
+            return held[1]
+        inv_lambda, qw, sw, bias = tensors
+        _need(qw.dim() == 2 + self.GROUPED, f"qw: {'[E, N, K]' if self.GROUPED else '[N, K]'} is needed, not {tuple(qw.shape)}")
+        lead, (N, K), device = tuple(qw.shape[:-2]), qw.shape[-2:], qw.device
+        _need_tensor("qw", qw, torch.int8, lead + (N, K), device)
+        _need_tensor("sw", sw, torch.float32, lead + (N,), device)
+        if inv_lambda is not None:
+            _need_tensor("inv_lambda", inv_lambda, torch.float32, lead + (K,), device)
+        if bias is not None:
+            _need_tensor("bias", bias, torch.float32, lead + (N,), device)
+        layer = _LayerInt8(lead[0] if lead else 0, N, K, _addr(inv_lambda), qw.data_ptr(), sw.data_ptr(), _addr(bias))
+        layer.address, layer.device = ctypes.addressof(layer), device
+        self._held = (tensors, layer)
+        return layer
+
+    def __getstate__(self):
+        """Copies make a descriptor of their own."""
+        return {**self.__dict__, "_held": None}
+
+    def _forward(self, x, rows, offsets, rho, row_rho, gelu, M, out):
+        layer = self._descriptor()
+        ldx = _need_rows("x", x, (torch.bfloat16,), (None, layer.K))
+        device = x.device
+        _need(device == layer.device, f"x is on {device}, the layer on {layer.device}")
+        if out is None:
+            y, ldy = torch.empty((M, layer.N), dtype=torch.bfloat16, device=device), layer.N
+        else:
+            _need(out.dtype == torch.bfloat16, "out: bfloat16 is needed")
+            y, ldy, _ = _linear_out(out, M, layer.N, None, device)
+        if M == 0:
+            return y
+        # codes and scales of this call alone, from torch's allocator: calls on other streams and captured ones have their own
+        work = torch.empty(M * (layer.K + 4), dtype=torch.uint8, device=device)
+        codes = work.data_ptr()
+        _check((_lib or load_library()).svdq_layer_int8_forward(
+            layer.address, x.data_ptr(), ldx, x.shape[0], _addr(rows), _addr(offsets), rho, _addr(row_rho), 1 if gelu else 0, M,
+            codes, codes + M * layer.K, y.data_ptr(), ldy, _raw_stream()), "svdq_layer_int8_forward")
+        return y
+
+
+class W8A8Linear(_W8A8):
+    """One linear in 8 bits: qw [N,K] int8, sw [N] f32 (weight n is qw[n] sw[n]), bias [N] f32 or None, and the smoothing vector inv_lambda [K]
+    f32 of its input, or None.  Holds references, lays nothing out, keeps no buffers: its calls may run on any streams at once."""
+    GROUPED = 0
+
+    def forward(self, x_bf16, rho=1.0, gelu=False, out=None):
+        """x [M,K] bf16 -> y [M,N] bf16: quantize_act_int8 and linear_w8a8 in one call.  out may share memory with x."""
+        return self._forward(x_bf16, None, None, float(rho), None, gelu, x_bf16.shape[0], out)
+
+
+class W8A8Experts(_W8A8):
+    """The linears of E experts: qw [E,N,K] int8, sw [E,N], bias [E,N] or None, inv_lambda [E,K] or None (f32)."""
+    GROUPED = 1
+
+    def forward(self, x_bf16, offsets, rho=1.0, rows=None, gelu=False, out=None):
+        """y [M,N] bf16 in the experts' order: rows offsets[e] .. offsets[e + 1] are expert e's, made of x[rows] (rows int32 [M]) or of x;
+        rho a number or every row's ratio (f32 [M]).  quantize_act_int8_grouped and linear_w8a8_grouped in one call; rows that no
+        expert owns are not written (without `out`: hold anything)."""
+        device = x_bf16.device
+        M = x_bf16.shape[0] if rows is None else rows.numel()
+        _need_tensor("offsets", offsets, torch.int32, (self.qw.shape[0] + 1,), device)
+        if rows is not None:
+            _need_tensor("rows", rows, torch.int32, (M,), device)
+        ratio, row_rho = _row_rho(rho, M, device)
+        return self._forward(x_bf16, rows, offsets, ratio, row_rho, gelu, M, out)

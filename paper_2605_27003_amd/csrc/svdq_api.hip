@@ -7,12 +7,14 @@
 #include <cmath>
 #include <cstring>
 
+#include "svdq_int8.h"
 #include "svdq_kernels.h"
 #include "svdq_mx_plan.h"
 
 namespace {
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // SVDQ_OK when the current device is gfx950; cached per device index.
 int check_arch() {
@@ -563,6 +565,87 @@ int svdq_layer_forward(const svdq_layer* L, const void* x_bf16, int64_t ldx, flo
         slices = 1;
     }
     return layer_gemm(L, act, scales, small, fields, expand, r ? hin : nullptr, r ? slices : 1, h, M, staging, y, ldy, stream);
+}
+
+// ---- the 8-bit layer.  Arguments of both forms; offsets null: not grouped.
+static int quantize_int8_check(const svdq::QuantInt8& q) {
+    if (!q.x || !q.qx || !q.sx || q.M < 0) return SVDQ_ERR_INVALID_ARG;
+    if (!q.row_rho && (!(q.rho > 0.0f) || !(q.rho <= 1.0f))) return SVDQ_ERR_INVALID_ARG;      // also rejects NaN
+    if (q.rows && q.x_rows < 0) return SVDQ_ERR_INVALID_ARG;
+    if (q.K <= 0 || q.K % 16 || q.K > SVDQ_MAX_K_INT8 || q.ldx < q.K || q.ldx % 8) return SVDQ_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(q.x) || !aligned16(q.inv_lambda) || !aligned16(q.qx) || !aligned4(q.sx) || !aligned4(q.rows) || !aligned4(q.row_rho))
+        return SVDQ_ERR_UNSUPPORTED_SHAPE;
+    return q.M > SVDQ_MAX_M ? SVDQ_ERR_UNSUPPORTED_SHAPE : SVDQ_OK;
+}
+
+static int gemm_int8_check(const svdq::GemmInt8& g, int out_dtype) {
+    if (!g.qx || !g.sx || !g.qw || !g.sw || !g.y || g.M < 0) return SVDQ_ERR_INVALID_ARG;
+    if (out_dtype != SVDQ_OUT_BF16 && out_dtype != SVDQ_OUT_F32) return SVDQ_ERR_INVALID_ARG;
+    if (g.N <= 0 || g.K <= 0 || g.K % 16 || g.K > SVDQ_MAX_K_INT8 || g.ldy < g.N) return SVDQ_ERR_UNSUPPORTED_SHAPE;
+    if (!aligned16(g.qx) || !aligned16(g.qw) || !aligned4(g.sx) || !aligned4(g.sw) || !aligned4(g.bias)) return SVDQ_ERR_UNSUPPORTED_SHAPE;
+    if ((uintptr_t)g.y & (out_dtype == SVDQ_OUT_F32 ? 3u : 1u)) return SVDQ_ERR_UNSUPPORTED_SHAPE;
+    if (g.M > SVDQ_MAX_M || !svdq::gemm_int8_fits(g)) return SVDQ_ERR_UNSUPPORTED_SHAPE;
+    return SVDQ_OK;
+}
+
+static int groups_check(const int32_t* offsets, int E) {
+    if (!offsets || E <= 0) return SVDQ_ERR_INVALID_ARG;
+    return E > SVDQ_MAX_EXPERTS || !aligned4(offsets) ? SVDQ_ERR_UNSUPPORTED_SHAPE : SVDQ_OK;
+}
+
+static int quantize_int8(const svdq::QuantInt8& q, int gelu, void* stream) {
+    if (int e = quantize_int8_check(q)) return e;
+    if (q.M == 0) return SVDQ_OK;
+    if (int a = check_arch()) return a;
+    return hip_status(svdq::launch_quantize_int8(q, gelu != 0, (hipStream_t)stream));
+}
+
+static int linear_int8(const svdq::GemmInt8& g, int out_dtype, void* stream) {
+    if (int e = gemm_int8_check(g, out_dtype)) return e;
+    if (g.M == 0) return SVDQ_OK;
+    if (int a = check_arch()) return a;
+    return hip_status(svdq::launch_gemm_int8(g, out_dtype == SVDQ_OUT_F32, (hipStream_t)stream));
+}
+
+int svdq_quantize_act_int8(const void* x_bf16, int64_t ldx, const float* inv_lambda, float rho, int gelu,
+                           int64_t M, int K, int8_t* qx, float* sx, void* stream) {
+    return quantize_int8(svdq::QuantInt8{x_bf16, ldx, nullptr, M, inv_lambda, nullptr, rho, K, M, qx, sx, {nullptr, 1}}, gelu, stream);
+}
+
+int svdq_linear_w8a8(const int8_t* qx, const float* sx, const int8_t* qw, const float* sw, const float* bias,
+                     int64_t M, int N, int K, void* y, int64_t ldy, int out_dtype, void* stream) {
+    return linear_int8(svdq::GemmInt8{qx, sx, qw, sw, bias, y, ldy, M, N, K, {nullptr, 1}}, out_dtype, stream);
+}
+
+int svdq_quantize_act_int8_grouped(const void* x_bf16, int64_t ldx, int64_t x_rows, const int32_t* rows,
+                                   const int32_t* offsets, int E, const float* inv_lambda, float rho, const float* row_rho, int gelu,
+                                   int64_t M, int K, int8_t* qx, float* sx, void* stream) {
+    if (int e = groups_check(offsets, E)) return e;
+    return quantize_int8(svdq::QuantInt8{x_bf16, ldx, rows, x_rows, inv_lambda, row_rho, rho, K, M, qx, sx, {offsets, E}}, gelu, stream);
+}
+
+int svdq_linear_w8a8_grouped(const int8_t* qx, const float* sx, const int8_t* qw, const float* sw, const float* bias,
+                             const int32_t* offsets, int E, int64_t M, int N, int K,
+                             void* y, int64_t ldy, int out_dtype, void* stream) {
+    if (int e = groups_check(offsets, E)) return e;
+    return linear_int8(svdq::GemmInt8{qx, sx, qw, sw, bias, y, ldy, M, N, K, {offsets, E}}, out_dtype, stream);
+}
+
+int svdq_layer_int8_forward(const svdq_layer_int8* L, const void* x_bf16, int64_t ldx, int64_t x_rows, const int32_t* rows,
+                            const int32_t* offsets, float rho, const float* row_rho, int gelu, int64_t M,
+                            int8_t* qx, float* sx, void* y, int64_t ldy, void* stream) {
+    if (!L || L->E < 0 || (L->E == 0 && (rows || offsets || row_rho))) return SVDQ_ERR_INVALID_ARG;
+    if (L->E)
+        if (int e = groups_check(offsets, L->E)) return e;
+    const svdq::Groups groups{offsets, L->E ? L->E : 1};
+    const svdq::QuantInt8 q{x_bf16, ldx, rows, x_rows, L->inv_lambda, row_rho, rho, L->K, M, qx, sx, groups};
+    const svdq::GemmInt8 g{qx, sx, L->qw, L->sw, L->bias, y, ldy, M, L->N, L->K, groups};
+    if (int e = quantize_int8_check(q)) return e;
+    if (int e = gemm_int8_check(g, SVDQ_OUT_BF16)) return e;
+    if (M == 0) return SVDQ_OK;
+    if (int a = check_arch()) return a;
+    const hipError_t e = svdq::launch_quantize_int8(q, gelu != 0, (hipStream_t)stream);
+    return hip_status(e != hipSuccess ? e : svdq::launch_gemm_int8(g, false, (hipStream_t)stream));
 }
 
 size_t svdq_gptq_workspace_bytes(int N, int K) {

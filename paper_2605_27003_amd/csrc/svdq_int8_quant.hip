@@ -1,0 +1,177 @@
+// Activations of the 8-bit layer: one pass over x that smooths (eq. 5), finds every token's largest magnitude, derives its clipped
+// scale s = (rho a) / 127 (eq. 8-9) and rounds its codes (eq. 3), K + 4 bytes written for 2 K read.
+//
+// A token's scale needs the whole row, so the row stays in registers between the maximum and the rounding: a wave, four or
+// sixteen of them share a row, eight consecutive k a lane and chunk.  The block walks a run of rows with the smoothing vector in
+// registers (it is twice a row's bytes) and the next row's x under way; one barrier a row where waves share it, on
+// two alternating sets of partial maxima.
+//
+// A row with a NaN or an infinity gets scale NaN and codes 0, so its outputs are NaN and no other row's are; a row whose
+// scale would not be a normal number gets scale 0 and codes 0.
+#include "svdq_act.h"
+#include "svdq_int8_dev.h"
+
+namespace svdq {
+
+namespace {
+
+// W waves share a row of up to 512 W C values; a block has four waves (W <= 4) or sixteen.
+template <int W, int C, bool GELU, bool GROUPED>
+__global__ __launch_bounds__(W <= 4 ? 256 : 64 * W)
+void quantize_int8_kernel(const QuantInt8 q, const int run) {
+    constexpr int NW = W <= 4 ? 4 : W, TEAMS = NW / W;               // teams of W waves, each with rows of its own
+    __shared__ uint32_t part[2][NW];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int team = wave / W, tw = wave % W;
+    const int chunks = q.K >> 3;
+    int at[C];                                                       // the lane's chunks; those past K repeat the last one
+    bool in[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int i = (c * W + tw) * 64 + lane;
+        in[c] = i < chunks;
+        at[c] = in[c] ? i : chunks - 1;
+    }
+    const int64_t begin = ((int64_t)blockIdx.x * TEAMS + team) * run;
+    const uint16_t* const x = reinterpret_cast<const uint16_t*>(q.x);
+
+    auto load = [&](uint4 (&v)[C], const int64_t row) {
+        int64_t r = row;
+        bool none = row >= q.M;
+        if (!none && q.rows) {
+            r = q.rows[row];
+            none = r < 0 || r >= q.x_rows;                           // no such token: zeros
+        }
+        if (none) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) v[c] = uint4{0, 0, 0, 0};
+            return;
+        }
+        const uint4* const p = reinterpret_cast<const uint4*>(x + r * q.ldx);
+#pragma unroll
+        for (int c = 0; c < C; ++c) v[c] = p[at[c]];
+    };
+    float il[C][8];
+    auto load_il = [&](const int e) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const float4v* const p = reinterpret_cast<const float4v*>(q.inv_lambda + (int64_t)e * q.K) + 2 * at[c];
+            const float4v a = p[0], b = p[1];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) il[c][i] = a[i], il[c][4 + i] = b[i];
+        }
+    };
+    uint4 next[C];
+    load(next, begin);
+    int expert = -1;
+    if (!GROUPED && q.inv_lambda) load_il(0);
+
+    for (int i = 0; i < run; ++i) {
+        const int64_t row = begin + i;
+        if (W == 1 && row >= q.M) return;                            // teams of one wave have no barrier to keep
+        uint4 v[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) v[c] = next[c];
+        if (i + 1 < run) load(next, row + 1);
+        bool owned = row < q.M;
+        if constexpr (GROUPED) {
+            if (owned) {
+                const int e = expert_of_row(q.groups, row, lane);
+                owned = e >= 0;
+                if (owned && e != expert && q.inv_lambda) load_il(e);
+                if (owned) expert = e;
+            }
+        }
+        float xs[C][8];
+        uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (GELU) w[j] = gelu_tanh_bf16x2(w[j]);
+                xs[c][2 * j] = bf16lo_f(w[j]);
+                xs[c][2 * j + 1] = bf16hi_f(w[j]);
+            }
+            if (q.inv_lambda)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) xs[c][j] = __fmul_rn(xs[c][j], il[c][j]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {                            // magnitudes as bit patterns: a NaN is the largest
+                const uint32_t m = f_bits(xs[c][j]) & 0x7fffffffu;
+                top = m > top ? m : top;
+            }
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t o = __shfl_xor(top, d);
+            top = o > top ? o : top;
+        }
+        if constexpr (W > 1) {
+            if (lane == 0) part[i & 1][wave] = top;
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < W; ++k) {
+                const uint32_t o = part[i & 1][team * W + k];
+                top = o > top ? o : top;
+            }
+        }
+        if (!owned) continue;
+        const bool finite = top < 0x7f800000u;
+        const float rho = q.row_rho ? q.row_rho[row] : q.rho;
+        float s = __fdiv_rn(__fmul_rn(rho, bits_f(top)), QMAX8);
+        const bool fine = finite && s >= 1.17549435e-38f;
+        const float inv = fine ? __fdiv_rn(1.0f, s) : 0.0f;
+        if (!fine) s = finite && s == s ? 0.0f : bits_f(0x7fc00000u);
+        if (lane == 0 && tw == 0) q.sx[row] = s;
+        int8_t* const out = q.qx + row * q.K;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            // clamped first, so that adding 1.5 2^23 rounds to the nearest whole number (ties to even) in the low bits
+            uint32_t b[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                b[j] = f_bits(__fadd_rn(__builtin_amdgcn_fmed3f(__fmul_rn(xs[c][j], inv), -QMAX8, QMAX8), 12582912.0f));
+            uint2 o;
+            o.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
+            o.y = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[7], b[6], 0x0c0c0400u), __builtin_amdgcn_perm(b[5], b[4], 0x0c0c0400u), 0x05040100u);
+            if (!fine) o = uint2{0, 0};
+            if (in[c]) reinterpret_cast<uint2*>(out)[at[c]] = o;
+        }
+    }
+}
+
+template <int W, int C>
+hipError_t launch_row(const QuantInt8& q, const bool gelu, hipStream_t stream) {
+    constexpr int TEAMS = W <= 4 ? 4 / W : 1, THREADS = W <= 4 ? 256 : 64 * W;
+    // eight blocks a CU, then longer runs of rows
+    int64_t run = q.M / (TEAMS * 2048);
+    run = run < 1 ? 1 : run > 16 ? 16 : run;
+    const int64_t blocks = (q.M + TEAMS * run - 1) / (TEAMS * run);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(THREADS), 0, stream, q, (int)run); };
+    if (q.groups.offsets) {
+        if (gelu) go(quantize_int8_kernel<W, C, true, true>);
+        else go(quantize_int8_kernel<W, C, false, true>);
+    } else {
+        if (gelu) go(quantize_int8_kernel<W, C, true, false>);
+        else go(quantize_int8_kernel<W, C, false, false>);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_quantize_int8(const QuantInt8& q, bool gelu, hipStream_t stream) {
+    const int chunks = q.K >> 3;
+    if (chunks <= 64) return launch_row<1, 1>(q, gelu, stream);
+    if (chunks <= 128) return launch_row<1, 2>(q, gelu, stream);
+    if (chunks <= 256) return launch_row<4, 1>(q, gelu, stream);
+    if (chunks <= 512) return launch_row<4, 2>(q, gelu, stream);
+    if (chunks <= 768) return launch_row<4, 3>(q, gelu, stream);
+    if (chunks <= 1024) return launch_row<4, 4>(q, gelu, stream);
+    if (chunks <= 2048) return launch_row<16, 2>(q, gelu, stream);
+    return launch_row<16, 4>(q, gelu, stream);
+}
+
+}  // namespace svdq
