@@ -2,9 +2,11 @@
 #pragma once
 #include "svdq_int8.h"
 #include "svdq_lds.h"
+#include "svdq_tiles.h"
 
 namespace svdq {
 
+constexpr int BK = 128;          // k (and bytes) of a row per stage of a product: one memory line
 constexpr float QMAX8 = 127.0f;  // codes are symmetric: -128 is not used
 
 // Expert of a row, or -1 for a row that no expert owns.  The running maximum of the offsets passes `row` where the first
@@ -87,6 +89,42 @@ __device__ __forceinline__ bool group_tile(const Groups& g, const int M, const i
     t.nt = rem / width;
     t.mt = 8 * sm + rem - t.nt * width;
     return true;
+}
+
+// Where a block's tile lies, and its expert's weights.
+struct TilePlace {
+    int m0, m_end, n0;
+    const int8_t* qw;
+    const float *sw, *bias;
+};
+template <int BM, int BN, bool GROUPED>
+__device__ __forceinline__ bool tile_place(const GemmInt8& g, const TileGrid& tg, const int id, const int lane, TilePlace& p) {
+    int mt, nt;
+    p.qw = g.qw;
+    p.sw = g.sw;
+    p.bias = g.bias;
+    if constexpr (GROUPED) {
+        GroupTile t;
+        if (!group_tile(g.groups, (int)g.M, BM, tg.ntiles, id, lane, t)) return false;
+        p.m0 = t.row0 + t.mt * BM;
+        p.m_end = t.row_end;
+        nt = t.nt;
+        p.qw += (int64_t)t.e * g.N * g.K;
+        p.sw += (int64_t)t.e * g.N;
+        if (p.bias) p.bias += (int64_t)t.e * g.N;
+    } else {
+        if (!tile_of(tg, id, mt, nt)) return false;
+        p.m0 = mt * BM;
+        p.m_end = (int)g.M;
+    }
+    p.n0 = nt * BN;
+    return true;
+}
+
+// As many blocks as there can be tiles: every expert with rows adds at most one row tile that is not full.
+inline int grouped_blocks(const GemmInt8& g, const int bm, const int bn) {
+    const int64_t mt = g.M / bm + (g.M < g.groups.E ? g.M : g.groups.E);
+    return (int)((mt * ((g.N + bn - 1) / bn) + 7) / 8 * 8);
 }
 
 }  // namespace svdq

@@ -17,236 +17,270 @@ namespace svdq {
 
 namespace {
 
-constexpr int BK = 128;                                   // k (and bytes) of a row per stage
-
-template <int BM_, int BN_, int WM_, int WN_, int NS_>
-struct Int8Tile {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NS = NS_, NW = WM * WN, THREADS = 64 * NW;
-    static constexpr int MT = BM / WM / 32, NT = BN / WN / 32;        // 32 x 32 blocks of a wave
-    static constexpr int ND = (BM + BN) / 8 / NW;                     // transfers of a wave per stage, eight rows each
-    static constexpr uint32_t STAGE = (BM + BN) * BK;
-    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "a transfer is of one operand");
+// The matrix instruction of a kernel: I x I results of 1024 / I k.  Lane l holds row l % I of an operand and 16 consecutive k (bytes), those
+// from 16 (l / I) on; of the results it holds column (token) l % I and QUADS runs of four rows (channels), the first at 4 (l / I), 8 apart.
+template <int I> struct Mfma;
+template <> struct Mfma<32> {
+    using Acc = int16v;
+    static constexpr int QUADS = 4;
+    static __device__ __forceinline__ Acc mul(int4v a, int4v b, Acc c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
+};
+template <> struct Mfma<16> {
+    using Acc = int4v;
+    static constexpr int QUADS = 1;
+    static __device__ __forceinline__ Acc mul(int4v a, int4v b, Acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 };
 
-// A wave's finished block row: 32 tokens x 32 NT channels, transposed through the wave's own LDS and stored 16 bytes a lane.
-// value(ni, i) is the lane's token's value of channel 32 ni + 8 (i / 4) + 4 (lane / 32) + i % 4.  `vec`: whole pieces can be stored
-// as 16 bytes; the pieces at N's end, and all of them otherwise, go element by element.
-template <class T, int NT, class Value>
-__device__ __forceinline__ void store_rows(Value value, const uint32_t region, const int lane, T* __restrict__ y, const int64_t ldy,
-                                           const int rows, const int cols, const bool vec) {
-    constexpr int ROW = NT * 32 * (int)sizeof(T), PITCH = ROW + 16, LANES = ROW / 16, STEP = 64 / LANES, EL = 16 / (int)sizeof(T);
-    const int l32 = lane & 31, kh = lane >> 5;
+// The end of a tile whose scales and biases stand in LDS (binary32: the tokens', the channels', the channels' biases): y = acc sx sw + bias,
+// up to 64 tokens at a time in column groups whose rows are one memory line (128 bytes) where the wave has as many channels, each
+// transposed through the wave's own LDS and stored 16 bytes a lane.  `vec`: whole pieces can be stored as 16 bytes; a piece over the
+// last channel, and every piece otherwise, goes element by element.
+template <class T, int I, int MT, int NT>
+struct TileStore {
+    static constexpr int EL = 16 / (int)sizeof(T), COLS = NT * I < 8 * EL ? NT * I : 8 * EL, ROWS = MT * I < 64 ? MT * I : 64;
+    static constexpr int PITCH = COLS * (int)sizeof(T) + 16, BYTES = ROWS * PITCH;
+    static constexpr int CB = COLS / I, MP = ROWS / I, LANES = COLS / EL, STEP = 64 / LANES;
+    static_assert(NT % CB == 0 && MT % MP == 0 && ROWS % STEP == 0, "whole groups");
+    // region: BYTES of the wave's own.  tokens, channels, biases: LDS addresses of the wave's first.
+    static __device__ __forceinline__ void run(const typename Mfma<I>::Acc (&acc)[NT][MT], const uint32_t region, const uint32_t tokens, const uint32_t channels, const uint32_t biases,
+                                               const bool has_bias, const int lane, T* __restrict__ y, const int64_t ldy, const int rows, const int cols, const bool vec) {
+        const int li = lane % I, lk = lane / I;
 #pragma unroll
-    for (int ni = 0; ni < NT; ++ni)
+        for (int m0 = 0; m0 < MT; m0 += MP) {
+            float ts[MP];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const uint32_t at = region + l32 * PITCH + (ni * 32 + 8 * q + 4 * kh) * (int)sizeof(T);
-            const float v0 = value(ni, 4 * q), v1 = value(ni, 4 * q + 1), v2 = value(ni, 4 * q + 2), v3 = value(ni, 4 * q + 3);
-            if constexpr (sizeof(T) == 2) {
-                lds_write8_pinned(at, uint2{f2_bf16_rne(v0, v1), f2_bf16_rne(v2, v3)});
-            } else {
-                lds_write8_pinned(at, uint2{f_bits(v0), f_bits(v1)});
-                lds_write8_pinned(at + 8, uint2{f_bits(v2), f_bits(v3)});
+            for (int mi = 0; mi < MP; ++mi) ts[mi] = bits_f(lds_read4(tokens + ((m0 + mi) * I + li) * 4));
+#pragma unroll
+            for (int g = 0; g < NT / CB; ++g) {
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                    for (int q = 0; q < Mfma<I>::QUADS; ++q) {
+                        const int ni = g * CB + cb, at = 8 * q + 4 * lk;
+                        const uint32_t c = (ni * I + at) * 4;
+                        const uint4 s4 = lds_read16(channels + c), b4 = has_bias ? lds_read16(biases + c) : uint4{0, 0, 0, 0};
+                        const float s[4] = {bits_f(s4.x), bits_f(s4.y), bits_f(s4.z), bits_f(s4.w)};
+                        const float b[4] = {bits_f(b4.x), bits_f(b4.y), bits_f(b4.z), bits_f(b4.w)};
+#pragma unroll
+                        for (int mi = 0; mi < MP; ++mi) {
+                            float v[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) v[i] = ((float)acc[ni][m0 + mi][4 * q + i] * ts[mi]) * s[i] + b[i];
+                            const uint32_t to = region + (mi * I + li) * PITCH + (cb * I + at) * (int)sizeof(T);
+                            if constexpr (sizeof(T) == 2) {
+                                lds_write8_pinned(to, uint2{f2_bf16_rne(v[0], v[1]), f2_bf16_rne(v[2], v[3])});
+                            } else {
+                                lds_write8_pinned(to, uint2{f_bits(v[0]), f_bits(v[1])});
+                                lds_write8_pinned(to + 8, uint2{f_bits(v[2]), f_bits(v[3])});
+                            }
+                        }
+                    }
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+                const int r0 = lane / LANES, c = lane % LANES, left = cols - g * COLS;
+                T* const y0 = y + g * COLS + c * EL;
+#pragma unroll
+                for (int it = 0; it < ROWS / STEP; ++it) {
+                    const int row = it * STEP + r0;
+                    const uint4 v = lds_read16_pinned(region + row * PITCH + c * 16);
+                    if (m0 * I + row >= rows) continue;
+                    T* const p = y0 + (int64_t)(m0 * I + row) * ldy;
+                    if (vec && (c + 1) * EL <= left) {
+                        *reinterpret_cast<uint4*>(p) = v;
+                    } else {
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int i = 0; i < EL; ++i)
+                            if (c * EL + i < left) {
+                                if constexpr (sizeof(T) == 2) p[i] = (T)(w[i >> 1] >> (16 * (i & 1)));
+                                else p[i] = w[i];
+                            }
+                    }
+                }
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
             }
         }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    const int r0 = lane / LANES, c = lane % LANES;
-#pragma unroll
-    for (int it = 0; it < 32 / STEP; ++it) {
-        const int row = it * STEP + r0;
-        const uint4 v = lds_read16_pinned(region + row * PITCH + c * 16);
-        if (row >= rows) continue;
-        T* const p = y + (int64_t)row * ldy + c * EL;
-        if (vec && (c + 1) * EL <= cols) {
-            *reinterpret_cast<uint4*>(p) = v;
-        } else {
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int i = 0; i < EL; ++i)
-                if (c * EL + i < cols) {
-                    if constexpr (sizeof(T) == 2) p[i] = (T)(w[i >> 1] >> (16 * (i & 1)));
-                    else p[i] = w[i];
-                }
-        }
     }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
+};
 
-// TAIL: K is no multiple of a stage.  The last stage's pieces beyond K repeat the row's last piece, and count as zeros in the
-// weights' operand.
+// A tile of BM tokens by BN channels for WM x WN waves; its operands stand in LDS from DEPTH stages ahead on.
+template <int BM_, int BN_, int WM_, int WN_, int DEPTH_>
+struct Int8Tile {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, DEPTH = DEPTH_, I = 16, NW = WM * WN, THREADS = 64 * NW, MT = BM / WM / I, NT = BN / WN / I;
+    static constexpr int NA = BM / 8 / NW, NB = BN / 8 / NW;          // transfers of a wave a stage, eight rows each
+    static constexpr uint32_t A = BM * BK, W = BN * BK, RING = (DEPTH + 1) * A + DEPTH * W;
+    static constexpr int TOKENS = (BM + 63) / 64 * 64, CHANNELS = (BN + 63) / 64 * 64;                // scales and biases come 64 at a time
+    static constexpr uint32_t SCALES = (TOKENS + 2 * CHANNELS) * 4;
+    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && DEPTH >= 2, "whole transfers");
+};
+
+// The tokens' rows of a stage, A(s), stand in a ring of DEPTH + 1 places, the channels', W(s), in one of DEPTH.  Stage s requests
+// A(s + DEPTH) during its first three quarters (its place has been free since the barrier of stage s - 1) and W(s + DEPTH) during its
+// last, where W(s) stood: requests that come all at once behind the barrier take longer than the instructions that they stand between
+// (with a place less and all of them there, 256 x 256 tiles took 6 % longer at K = 13824).
 template <class G, bool TAIL, bool GROUPED, class T>
 __global__ __launch_bounds__(G::THREADS, 1)
 void gemm_int8_kernel(const GemmInt8 g, const TileGrid tg) {
-    constexpr int BM = G::BM, BN = G::BN, MT = G::MT, NT = G::NT, NS = G::NS, ND = G::ND, NW = G::NW;
-    constexpr int STORE = 32 * (NT * 32 * 4 + 16);                    // of a wave, the wider type's
-    constexpr uint32_t RING = NS * G::STAGE, BYTES = RING > NW * STORE ? RING : NW * STORE;
-    __shared__ __attribute__((aligned(16))) uint8_t ring[BYTES];
+    constexpr int BM = G::BM, BN = G::BN, MT = G::MT, NT = G::NT, NA = G::NA, NB = G::NB, I = G::I, DEPTH = G::DEPTH;
+    using Acc = typename Mfma<I>::Acc;
+    using Store = TileStore<T, I, MT, NT>;
+    static_assert(G::RING >= (G::NW + 1) * Store::BYTES + G::SCALES && G::A >= G::SCALES, "the store transposes in the ring, beside the scales");
+    __shared__ __attribute__((aligned(16))) uint8_t ring[G::RING];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % G::WM, wn = wave / G::WM;
-    const int l32 = lane & 31, kh = lane >> 5;
+    const int li = lane % I, lk = lane / I;
     const int K = g.K, N = g.N;
-    const uint32_t ring0 = (uint32_t)(uintptr_t)(lds_byte*)ring;
-
-    int m0, m_end, n0;
-    const int8_t* qw = g.qw;
-    const float *sw = g.sw, *bias = g.bias;
-    if constexpr (GROUPED) {
-        GroupTile t;
-        if (!group_tile(g.groups, (int)g.M, BM, tg.ntiles, blockIdx.x, lane, t)) return;
-        m0 = t.row0 + t.mt * BM;
-        m_end = t.row_end;
-        n0 = t.nt * BN;
-        qw += (int64_t)t.e * N * K;
-        sw += (int64_t)t.e * N;
-        if (bias) bias += (int64_t)t.e * N;
-    } else {
-        int mt, nt;
-        if (!tile_of(tg, blockIdx.x, mt, nt)) return;
-        m0 = mt * BM;
-        m_end = (int)g.M;
-        n0 = nt * BN;
-    }
+    const uint32_t ring_a = (uint32_t)(uintptr_t)(lds_byte*)ring, ring_w = ring_a + (DEPTH + 1) * G::A;
+    TilePlace at;
+    if (!tile_place<BM, BN, GROUPED>(g, tg, blockIdx.x, lane, at)) return;
+    const int m0 = at.m0, m_end = at.m_end, n0 = at.n0;
     const int nstages = (K + BK - 1) / BK;
 
-    // ---- transfers: number j of this wave covers rows 8 j .. 8 j + 7 of the tile's tokens, then of its channels
+    // ---- transfers: j of this wave covers rows 8 (wave NA + j) .. + 7
     const int8_t* const abase = g.qx + (int64_t)m0 * K;
-    const int8_t* const wbase = qw + (int64_t)n0 * K;
+    const int8_t* const wbase = at.qw + (int64_t)n0 * K;
     const int place = lane & 7;
-    uint32_t voff[ND], piece[2];
-    piece[0] = place ^ (lane >> 4);
-    piece[1] = place ^ (4 + (lane >> 4));
+    uint32_t va[NA], vw[NB], pa[NA], pw[NB];
+    auto rows_of = [&](uint32_t& v, uint32_t& piece, const int block, const int last) {              // rows past the end repeat the last one
+        const int row = 8 * block + (lane >> 3);
+        piece = place ^ ((row >> 1) & 7);
+        v = (uint32_t)(row < last ? row : last) * (uint32_t)K + piece * 16;
+    };
 #pragma unroll
-    for (int p = 0; p < ND; ++p) {
-        const int j = wave * ND + p;
-        const bool w = 8 * j >= BM;
-        const int left = (w ? N - 1 - n0 : m_end - 1 - m0);           // rows past the end repeat the last one
-        int row = 8 * j - (w ? BM : 0) + (lane >> 3);
-        row = row < left ? row : left;
-        voff[p] = (uint32_t)row * (uint32_t)K + piece[j & 1] * 16;
-    }
-    auto request = [&](const int s, const uint32_t slot, const int p) {
-        const int j = wave * ND + p;
-        const int8_t* const base = (8 * j >= BM ? wbase : abase) + (int64_t)s * BK;
-        uint32_t v = voff[p];
+    for (int j = 0; j < NA; ++j) rows_of(va[j], pa[j], wave * NA + j, m_end - 1 - m0);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) rows_of(vw[j], pw[j], wave * NB + j, N - 1 - n0);
+    auto request = [&](const int8_t* base, uint32_t v, const uint32_t piece, const int s, const uint32_t to) {
         if constexpr (TAIL) {
-            const int left = (K >> 4) - 8 * s - 1, over = (int)piece[j & 1] - left;
+            const int left = (K >> 4) - 8 * s - 1, over = (int)piece - left;
             if (over > 0) v -= over * 16;
         }
-        dma16(base, v, slot + j * 1024);
+        dma16(base + (int64_t)s * BK, v, to);
     };
+    auto request_a = [&](const int s, const uint32_t to, const int j) { request(abase, va[j], pa[j], s, to + (wave * NA + j) * 1024); };
+    auto request_w = [&](const int s, const uint32_t to, const int j) { request(wbase, vw[j], pw[j], s, to + (wave * NB + j) * 1024); };
+    auto next_a = [&](const uint32_t c) { return c == ring_a + DEPTH * G::A ? ring_a : c + G::A; };
+    auto next_w = [&](const uint32_t c) { return c == ring_w + (DEPTH - 1) * G::W ? ring_w : c + G::W; };
 
-    // ---- operands: piece 2 kk + kh of a row for k step kk
-    const uint32_t turn = (kh ^ (l32 >> 1)) & 7;
-    const uint32_t rd_a = (wm * MT * 32 + l32) * BK, rd_w = (BM + wn * NT * 32 + l32) * BK;
+    // ---- operands: piece PS kk + lk of a row, for k step kk, stands at that place ^ (row / 2) % 8
+    constexpr int PS = 64 / I, STEPS = 8 / PS;
+    const uint32_t turn = (lk ^ (li >> 1)) & 7;
+    uint32_t rd_a[STEPS], rd_w[STEPS];
+#pragma unroll
+    for (int kk = 0; kk < STEPS; ++kk) {
+        rd_a[kk] = (wm * MT * I + li) * BK + ((turn ^ (PS * kk)) << 4);
+        rd_w[kk] = (wn * NT * I + li) * BK + ((turn ^ (PS * kk)) << 4);
+    }
     struct Operands {
-        uint4 w[NT], x[MT];
+        int4v w[NT], x[MT];
     };
-    auto read_w = [&](Operands& o, const uint32_t slot, const int s, const int kk, const int ni) {
-        uint4 v = lds_read16_pinned(slot + rd_w + ni * 32 * BK + ((turn ^ (2 * kk)) << 4));
-        if constexpr (TAIL) {
-            if (8 * s + 2 * kk + kh >= (K >> 4)) v = uint4{0, 0, 0, 0};
+    typedef const volatile __attribute__((address_space(3))) int4v lds_i4;
+    auto fetch = [&](const uint32_t from, const int block) { return *reinterpret_cast<lds_i4*>((lds_byte*)(uintptr_t)from + block * I * BK); };
+    auto read = [&](Operands& o, const uint32_t fa, const uint32_t fw, const int s, const int kk, const int r) {
+        if (r >= 1 && r <= MT) {                                      // in the order of their use
+            o.x[r - 1] = fetch(fa, r - 1);
+            return;
         }
-        o.w[ni] = v;
+        const int ni = r == 0 ? 0 : r - MT;
+        o.w[ni] = fetch(fw, ni);
+        if constexpr (TAIL) {
+            if (8 * s + PS * kk + lk >= (K >> 4)) o.w[ni] = int4v{0, 0, 0, 0};
+        }
     };
-    auto read_x = [&](Operands& o, const uint32_t slot, const int kk, const int mi) {
-        o.x[mi] = lds_read16_pinned(slot + rd_a + mi * 32 * BK + ((turn ^ (2 * kk)) << 4));
-    };
-    auto next_slot = [&](const uint32_t c) { return (c == ring0 + (NS - 1) * G::STAGE) ? ring0 : c + G::STAGE; };
 
-    int16v acc[NT][MT];
+    Acc acc[NT][MT];
 #pragma unroll
     for (int ni = 0; ni < NT; ++ni)
 #pragma unroll
-        for (int mi = 0; mi < MT; ++mi) acc[ni][mi] = (int16v)(0);
+        for (int mi = 0; mi < MT; ++mi) acc[ni][mi] = (Acc)(0);
 
-    uint32_t cur = ring0;
-    {
-        uint32_t sl = ring0;
-        for (int s = 0; s < NS; ++s) {
-            if (s < nstages)
+    uint32_t cur_a = ring_a, cur_w = ring_w;
 #pragma unroll
-                for (int p = 0; p < ND; ++p) request(s, sl, p);
-            sl = next_slot(sl);
+    for (int s = 0; s < DEPTH; ++s)
+        if (s < nstages) {
+#pragma unroll
+            for (int j = 0; j < NA; ++j) request_a(s, ring_a + s * G::A, j);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) request_w(s, ring_w + s * G::W, j);
         }
-        if (nstages >= NS) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 1) * ND) : "memory");
+    // wait for a stage with `behind` whole ones, at most DEPTH - 1, requested after it
+    auto wait_for = [&](const int behind) {
+        if (DEPTH > 3 && behind >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * (NA + NB)) : "memory");
+        else if (DEPTH > 2 && behind == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (NA + NB)) : "memory");
+        else if (behind == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NA + NB) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    }
-    Operands op0, op1;
-#pragma unroll
-    for (int ni = 0; ni < NT; ++ni) read_w(op0, cur, 0, 0, ni);
-#pragma unroll
-    for (int mi = 0; mi < MT; ++mi) read_x(op0, cur, 0, mi);
-
-    // One k step: the products of `o`, and between them the reads of the next step's operands into `on` and, where the stage's slot
-    // has become free, the requests that fill it again.
-    auto step = [&](const Operands& o, Operands& on, const uint32_t slot, const int s, const int kk, const bool fetch, const bool refill,
-                    const int rs, const uint32_t rslot) {
-        constexpr int T_ = MT * NT, READS = MT + NT, RP = (READS + T_ - 1) / T_, DP = (ND + T_ - 1) / T_;
-#pragma unroll
-        for (int t = 0; t < T_; ++t) {
-            const int ni = t / MT, mi = t % MT;
-            const int4v a = {(int)o.w[ni].x, (int)o.w[ni].y, (int)o.w[ni].z, (int)o.w[ni].w};
-            const int4v b = {(int)o.x[mi].x, (int)o.x[mi].y, (int)o.x[mi].z, (int)o.x[mi].w};
-            acc[ni][mi] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, acc[ni][mi], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-            if (fetch)
-#pragma unroll
-                for (int r = t * RP; r < (t + 1) * RP && r < READS; ++r) {
-                    if (r == 0) read_w(on, slot, s, kk, 0);           // in the order of their use
-                    else if (r <= MT) read_x(on, slot, kk, r - 1);
-                    else read_w(on, slot, s, kk, r - MT);
-                }
-            if (refill)
-#pragma unroll
-                for (int p = t * DP; p < (t + 1) * DP && p < ND; ++p) request(rs, rslot, p);
-            __builtin_amdgcn_sched_barrier(0);
-        }
     };
-    // A stage: the wait for the next one and the barrier stand in front of its last step, when every wave has taken its last
-    // operands of this one out of LDS; that step's instructions carry the requests for stage s + NS.
-    auto stage = [&](const int s, const bool refill, const bool last) {
-        step(op0, op1, cur, s, 1, true, false, 0, 0);
-        step(op1, op0, cur, s, 2, true, false, 0, 0);
-        step(op0, op1, cur, s, 3, true, false, 0, 0);
-        if (refill) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NS - 2) * ND) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    static_assert(DEPTH <= 4, "wait_for");
+    wait_for((nstages < DEPTH ? nstages : DEPTH) - 1);
+    __syncthreads();
+    constexpr int T_ = MT * NT, READS = MT + NT, QUARTER = STEPS * T_ / 4;
+    Operands op[2];
+#pragma unroll
+    for (int r = 0; r < READS; ++r) read(op[0], ring_a + rd_a[0], ring_w + rd_w[0], 0, 0, r);
+
+    // A stage is STEPS k steps, of T_ instructions each; between those the reads of the next step's operands and the stage's requests.
+    // Before its last quarter (when every wave has all of its operands) stand the wait for the next stage's rows and the barrier.
+    auto stage = [&](const int s, auto FILLC, auto LASTC) {
+        constexpr bool fill = decltype(FILLC)::value, last = decltype(LASTC)::value;
+        const uint32_t na = next_a(cur_a), nw = next_w(cur_w), free_a = cur_a == ring_a ? ring_a + DEPTH * G::A : cur_a - G::A;
+        auto instructions = [&](auto FROM, auto TO) {
+            constexpr int from = decltype(FROM)::value, until = decltype(TO)::value, kk = from / T_, rk = (kk + 1) % STEPS;
+            constexpr bool next = kk + 1 == STEPS;                    // its reads are of the next stage, behind the barrier
+            constexpr int r0 = next ? 3 * QUARTER : kk * T_, span = next ? QUARTER : T_, RP = (READS + span - 1) / span;
+            uint32_t fa = (next ? na : cur_a) + rd_a[rk], fw = (next ? nw : cur_w) + rd_w[rk];
+            asm volatile("" : "+v"(fa), "+v"(fw));
+#pragma unroll
+            for (int n = from; n < until; ++n) {
+                const int t = n % T_, ni = t / MT, mi = t % MT;
+                acc[ni][mi] = Mfma<I>::mul(op[kk & 1].w[ni], op[kk & 1].x[mi], acc[ni][mi]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (!(next && last) && n >= r0)
+#pragma unroll
+                    for (int r = (n - r0) * RP; r < (n - r0 + 1) * RP && r < READS; ++r)
+                        read(op[rk & 1], fa, fw, next ? s + 1 : s, rk, r);
+                if constexpr (fill) {                                 // request i of n stands behind instruction (i + 1/2) / n of its part
+#pragma unroll
+                    for (int j = 0; j < NA; ++j)
+                        if (n == (2 * j + 1) * 3 * QUARTER / (2 * NA)) request_a(s + DEPTH, free_a, j);
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+                        if (n == 3 * QUARTER + j * QUARTER / NB) request_w(s + DEPTH, cur_w, j);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        instructions(IC<0>{}, IC<T_>{});
+        instructions(IC<T_>{}, IC<3 * QUARTER>{});
+        if constexpr (fill) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 2) * (NA + NB) + NA) : "memory");
+        else wait_for(nstages - 2 - s);
         __syncthreads();
-        const uint32_t nxt = next_slot(cur);
-        step(op1, op0, nxt, s + 1, 0, !last, refill, s + NS, cur);
-        cur = nxt;
+        instructions(IC<3 * QUARTER>{}, IC<4 * QUARTER>{});
+        cur_a = na;
+        cur_w = nw;
     };
     int s = 0;
-    for (; s + NS < nstages; ++s) stage(s, true, false);
-    for (; s + 1 < nstages; ++s) stage(s, false, false);
-    stage(s, false, true);
-
-    // ---- y = acc sx sw + bias, one block row at a time.  The barrier of the last stage was passed when every wave had read its
-    // last operands: the ring is free.
-    const bool vec = ((reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)(g.ldy * (int64_t)sizeof(T))) & 15) == 0;
-    const int nw = n0 + wn * NT * 32;
-    if (nw >= N) return;
-    float cs[NT][16], cb[NT][16];
-#pragma unroll
-    for (int ni = 0; ni < NT; ++ni)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int n = nw + 32 * ni + 8 * (i >> 2) + 4 * kh + (i & 3), at = n < N ? n : N - 1;
-            cs[ni][i] = sw[at];
-            cb[ni][i] = bias ? bias[at] : 0.0f;
-        }
-#pragma unroll
-    for (int mi = 0; mi < MT; ++mi) {
-        const int m = m0 + (wm * MT + mi) * 32, rows = m_end - m;
-        if (rows <= 0) break;
-        const float ts = g.sx[l32 < rows ? m + l32 : m_end - 1];
-        store_rows<T, NT>([&](const int ni, const int i) { return ((float)acc[ni][mi][i] * ts) * cs[ni][i] + cb[ni][i]; },
-                          ring0 + wave * STORE, lane, reinterpret_cast<T*>(g.y) + (int64_t)m * g.ldy + nw, g.ldy, rows, N - nw, vec);
+    for (; s + DEPTH < nstages; ++s) stage(s, IC<1>{}, IC<0>{});
+    for (; s + 1 < nstages; ++s) stage(s, IC<0>{}, IC<0>{});
+    // the last stage's requests are the tile's scales and biases, 64 values each, into the place behind its tokens'
+    const uint32_t scales = next_a(cur_a);
+    for (int j = wave; j < (int)G::SCALES / 256; j += G::NW) {
+        constexpr int CHANNEL0 = G::TOKENS / 64, BIAS0 = CHANNEL0 + G::CHANNELS / 64;
+        const bool tok = j < CHANNEL0, bia = j >= BIAS0;
+        const int i = (j - (tok ? 0 : bia ? BIAS0 : CHANNEL0)) * 64 + lane, end = tok ? m_end - 1 - m0 : N - 1 - n0;
+        if (!bia || at.bias) dma4(tok ? g.sx + m0 : bia ? at.bias + n0 : at.sw + n0, (uint32_t)(i < end ? i : end) * 4, scales + j * 256);
     }
+    stage(s, IC<0>{}, IC<1>{});
+
+    const bool vec = ((reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)(g.ldy * (int64_t)sizeof(T))) & 15) == 0;
+    const int mw = m0 + wm * MT * I, nw = n0 + wn * NT * I;
+    if (nw >= N || mw >= m_end) return;
+    const int below = (int)(scales - ring_a) / Store::BYTES;          // waves whose store area fits below the scales
+    const uint32_t region = wave < below ? ring_a + wave * Store::BYTES : scales + G::SCALES + (wave - below) * Store::BYTES;
+    Store::run(acc, region, scales + wm * MT * I * 4, scales + (G::TOKENS + wn * NT * I) * 4, scales + (G::TOKENS + G::CHANNELS + wn * NT * I) * 4,
+               at.bias != nullptr, lane, reinterpret_cast<T*>(g.y) + (int64_t)mw * g.ldy + nw, g.ldy, m_end - mw, N - nw, vec);
 }
 
 template <class G, bool TAIL, bool GROUPED>
@@ -255,19 +289,12 @@ void launch_tiles_t(const GemmInt8& g, const bool out_f32, const TileGrid& tg, c
     else hipLaunchKernelGGL((gemm_int8_kernel<G, TAIL, GROUPED, uint16_t>), dim3(blocks), dim3(G::THREADS), 0, stream, g, tg);
 }
 
-// As many blocks as there can be tiles: every expert with rows adds at most one row tile that is not full.
-template <class G>
-int64_t grouped_blocks(const GemmInt8& g) {
-    const int64_t mt = g.M / G::BM + (g.M < g.groups.E ? g.M : g.groups.E);
-    return (mt * ((g.N + G::BN - 1) / G::BN) + 7) / 8 * 8;
-}
-
 template <class G>
 hipError_t launch_tiles(const GemmInt8& g, const bool out_f32, hipStream_t stream) {
     const int ntiles = (g.N + G::BN - 1) / G::BN;
     const bool tail = g.K % BK != 0;
     if (g.groups.offsets) {
-        const int blocks = (int)grouped_blocks<G>(g);
+        const int blocks = (int)grouped_blocks(g, G::BM, G::BN);
         const TileGrid tg{0, ntiles, 0, 0};
         if (tail) launch_tiles_t<G, true, true>(g, out_f32, tg, blocks, stream);
         else launch_tiles_t<G, false, true>(g, out_f32, tg, blocks, stream);
@@ -279,16 +306,34 @@ hipError_t launch_tiles(const GemmInt8& g, const bool out_f32, hipStream_t strea
     return hipGetLastError();
 }
 
-using T128 = Int8Tile<128, 128, 2, 2, 2>;
+using T256 = Int8Tile<256, 256, 2, 4, 2>;
+using T128 = Int8Tile<128, 128, 2, 4, 4>;
+using T64 = Int8Tile<64, 64, 2, 2, 4>;
 
 }  // namespace
 
-// Block ids and tile numbers are 32-bit: rounded up to the eight XCDs, fewer than 2^31 / 8 row tiles of eight by channel tiles.
+// Tiles are chosen by the rows that there are (an expert, on average).
+enum class Int8Plan { FEW, T64, T128, T256 };
+static Int8Plan plan(const GemmInt8& g) {
+    const int64_t rows = g.groups.offsets ? (g.M + g.groups.E - 1) / g.groups.E : g.M;
+    return rows <= 64 ? Int8Plan::FEW : rows <= 256 ? Int8Plan::T64 : rows <= 1024 ? Int8Plan::T128 : Int8Plan::T256;
+}
+
+// Block ids and tile numbers are 32-bit.
 bool gemm_int8_fits(const GemmInt8& g) {
-    const int64_t mt = (g.M + 127) / 128 + (g.groups.offsets ? g.groups.E : 0), nt = ((int64_t)g.N + 127) / 128;
+    const Int8Plan p = plan(g);
+    const int bm = p == Int8Plan::T256 ? 256 : p == Int8Plan::T128 ? 128 : p == Int8Plan::T64 ? 64 : 16, bn = bm;
+    const int64_t mt = (g.M + bm - 1) / bm + (g.groups.offsets ? g.groups.E : 0), nt = ((int64_t)g.N + bn - 1) / bn;
     return (mt + 8) * (nt + 8) < INT32_MAX;
 }
 
-hipError_t launch_gemm_int8(const GemmInt8& g, bool out_f32, hipStream_t stream) { return launch_tiles<T128>(g, out_f32, stream); }
+hipError_t launch_gemm_int8(const GemmInt8& g, bool out_f32, hipStream_t stream) {
+    switch (plan(g)) {
+        case Int8Plan::FEW: return launch_gemm_int8_few(g, (int)(g.groups.offsets ? (g.M + g.groups.E - 1) / g.groups.E : g.M), out_f32, stream);
+        case Int8Plan::T64: return launch_tiles<T64>(g, out_f32, stream);
+        case Int8Plan::T128: return launch_tiles<T128>(g, out_f32, stream);
+        default: return launch_tiles<T256>(g, out_f32, stream);
+    }
+}
 
 }  // namespace svdq
