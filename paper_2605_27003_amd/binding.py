@@ -682,128 +682,141 @@ class W4A4Linear:
 
 
 # ---- the 8-bit layer, and its form grouped by expert ---------------------------------------------
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+# Arguments are checked here for what the C functions cannot see (types, shapes, devices): a few comparisons a tensor, words only
+# where one fails, since calls with few tokens wait for the host.
+def _gpu(t):
+    """The GPU that holds t, which has to be the current one."""
+    gpu = t.get_device()
+    if gpu >= 0:
+        try:
+            current = torch._C._cuda_getDevice()
+        except AttributeError:
+            current = torch.cuda.current_device()
+        if gpu == current:
+            return gpu
+    raise ValueError(f"tensors on the current GPU are needed, not on {t.device}")
 
 
-def _need_tensor(name, t, dtype, shape, device):
-    """A contiguous GPU tensor of the type and shape that the kernels read (None in a shape: any size)."""
-    _need(t.dtype == dtype and t.dim() == len(shape) and all(w is None or w == n for w, n in zip(shape, t.shape)) and t.is_contiguous(),
-          f"{name}: a contiguous {dtype} tensor of shape {tuple('any' if n is None else n for n in shape)} is needed, not {t.dtype} {tuple(t.shape)}")
-    _need(t.device == device, f"{name} is on {t.device}, not on {device}")
+def _refuse(name, t, dtype, shape, gpu):
+    wanted = " or ".join(map(str, dtype)) if isinstance(dtype, tuple) else dtype
+    raise ValueError(f"{name}: {wanted} of shape {shape} is needed, rows of consecutive values, on GPU {gpu} (the current one); "
+                     f"got {t.dtype} of shape {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
 
 
-def _need_rows(name, t, dtypes, shape):
-    """A matrix whose rows may be further apart than they are long, on the current GPU; returns its row stride."""
-    _need(t.dim() == 2 and t.dtype in dtypes and all(w is None or w == n for w, n in zip(shape, t.shape)),
-          f"{name}: {' or '.join(map(str, dtypes))} of shape {tuple('any' if n is None else n for n in shape)} is needed, not {t.dtype} {tuple(t.shape)}")
-    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), f"{name} is on {t.device}, not on the current GPU")
+def _vector(name, t, dtype, shape, gpu):
+    """A contiguous tensor of this type and shape on GPU `gpu` -> its address."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != gpu or not t.is_contiguous():
+        _refuse(name, t, dtype, shape, gpu)
+    return t.data_ptr()
+
+
+def _optional(name, t, dtype, shape, gpu):
+    return None if t is None else _vector(name, t, dtype, shape, gpu)
+
+
+def _matrix(name, t, dtypes, gpu, cols=None):
+    """A matrix on GPU `gpu` whose rows of consecutive values may be further apart than they are long -> (rows, columns, row stride)."""
+    if t.dim() != 2 or t.dtype not in dtypes or t.get_device() != gpu or (cols is not None and t.shape[1] != cols):
+        _refuse(name, t, dtypes, ("any", "any" if cols is None else cols), gpu)
     rows, cols = t.shape
-    _need((cols <= 1 or t.stride(1) == 1) and (rows <= 1 or t.stride(0) >= cols), f"{name}: rows of consecutive values are needed")
-    return t.stride(0) if rows > 1 else max(cols, (cols + 7) & ~7)
+    if rows <= 1:
+        ld = (cols + 7) & ~7
+    else:
+        ld = t.stride(0)
+        if ld < cols:
+            _refuse(name, t, dtypes, (rows, cols), gpu)
+    if cols > 1 and t.stride(1) != 1:
+        _refuse(name, t, dtypes, (rows, cols), gpu)
+    return rows, cols, ld
 
 
-def _quantize_int8_out(out, M, K, device):
+_BF16, _F32, _I8, _I32 = torch.bfloat16, torch.float32, torch.int8, torch.int32
+
+
+def _quantize_int8_out(out, M, K, x, gpu):
     if out is None:
-        return torch.empty((M, K), dtype=torch.int8, device=device), torch.empty(M, dtype=torch.float32, device=device)
-    _need_tensor("out[0]", out[0], torch.int8, (M, K), device)
-    _need_tensor("out[1]", out[1], torch.float32, (M,), device)
+        return torch.empty((M, K), dtype=_I8, device=x.device), torch.empty(M, dtype=_F32, device=x.device)
+    _vector("out[0]", out[0], _I8, (M, K), gpu)
+    _vector("out[1]", out[1], _F32, (M,), gpu)
     return out
 
 
 def quantize_act_int8(x_bf16, inv_lambda=None, rho=1.0, gelu=False, out=None):
     """x [M,K] bf16 (row stride allowed) -> (qx [M,K] int8, sx [M] f32): codes of x * inv_lambda (None: of x) with one scale
     (rho max|.|) / 127 a token; gelu=True: of gelu(x)."""
-    ldx = _need_rows("x", x_bf16, (torch.bfloat16,), (None, None))
-    M, K = x_bf16.shape
-    if inv_lambda is not None:
-        _need_tensor("inv_lambda", inv_lambda, torch.float32, (K,), x_bf16.device)
-    qx, sx = _quantize_int8_out(out, M, K, x_bf16.device)
-    if M == 0:                       # an empty tensor has no address
-        return qx, sx
-    _check(load_library().svdq_quantize_act_int8(_ptr(x_bf16), ldx, _ptr(inv_lambda), float(rho), int(bool(gelu)), M, K,
-                                                 _ptr(qx), _ptr(sx), _stream()), "svdq_quantize_act_int8")
+    gpu = _gpu(x_bf16)
+    M, K, ldx = _matrix("x", x_bf16, (_BF16,), gpu)
+    il = _optional("inv_lambda", inv_lambda, _F32, (K,), gpu)
+    qx, sx = _quantize_int8_out(out, M, K, x_bf16, gpu)
+    if M:                            # an empty tensor has no address
+        _check((_lib or load_library()).svdq_quantize_act_int8(x_bf16.data_ptr(), ldx, il, float(rho), 1 if gelu else 0, M, K, qx.data_ptr(), sx.data_ptr(),
+                                                               _raw_stream()), "svdq_quantize_act_int8")
     return qx, sx
 
 
-def _linear_out(out, M, N, out_dtype, device):
+def _linear_out(out, M, N, out_dtype, like, gpu):
     """(y, its row stride, its type's code)"""
     if out is None:
-        _need(out_dtype in (torch.bfloat16, torch.float32), f"out_dtype: bfloat16 or float32, not {out_dtype}")
-        out = torch.empty((M, N), dtype=out_dtype, device=device)
-    else:
-        _need(out.device == device, f"out is on {out.device}, not on {device}")
-        _need_rows("out", out, (torch.bfloat16, torch.float32), (M, N))
-    return out, out.stride(0) if M > 1 else N, OUT_F32 if out.dtype == torch.float32 else OUT_BF16
+        if out_dtype is not _BF16 and out_dtype is not _F32:
+            raise ValueError(f"out_dtype: bfloat16 or float32, not {out_dtype}")
+        return torch.empty((M, N), dtype=out_dtype, device=like.device), N, OUT_F32 if out_dtype is _F32 else OUT_BF16
+    rows, _, ldy = _matrix("out", out, (_BF16, _F32), gpu, N)
+    if rows != M:
+        _refuse("out", out, (_BF16, _F32), (M, N), gpu)
+    return out, ldy, OUT_F32 if out.dtype is _F32 else OUT_BF16
 
 
 def linear_w8a8(qx, sx, qw, sw, bias=None, out=None, out_dtype=torch.bfloat16):
     """qx [M,K] int8, sx [M] f32, qw [N,K] int8, sw [N] f32, bias [N] f32 -> y [M,N] = (qx qw^T) sx sw + bias, bf16 or f32."""
-    _need_rows("qx", qx, (torch.int8,), (None, None))
-    (M, K), N, device = qx.shape, qw.shape[0], qx.device
-    _need(qx.is_contiguous(), "qx: a contiguous tensor is needed")
-    _need_tensor("sx", sx, torch.float32, (M,), device)
-    _need_tensor("qw", qw, torch.int8, (None, K), device)
-    _need_tensor("sw", sw, torch.float32, (N,), device)
-    if bias is not None:
-        _need_tensor("bias", bias, torch.float32, (N,), device)
-    y, ldy, code = _linear_out(out, M, N, out_dtype, device)
-    if M == 0:
-        return y
-    _check(load_library().svdq_linear_w8a8(_ptr(qx), _ptr(sx), _ptr(qw), _ptr(sw), _ptr(bias), M, N, K, _ptr(y), ldy, code, _stream()),
-           "svdq_linear_w8a8")
+    gpu = _gpu(qx)
+    if qx.dim() != 2 or qw.dim() != 2:
+        _refuse("qx, qw", qx if qx.dim() != 2 else qw, _I8, ("any", "any"), gpu)
+    (M, K), N = qx.shape, qw.shape[0]
+    args = (_vector("qx", qx, _I8, (M, K), gpu), _vector("sx", sx, _F32, (M,), gpu), _vector("qw", qw, _I8, (N, K), gpu),
+            _vector("sw", sw, _F32, (N,), gpu), _optional("bias", bias, _F32, (N,), gpu))
+    y, ldy, code = _linear_out(out, M, N, out_dtype, qx, gpu)
+    if M:
+        _check((_lib or load_library()).svdq_linear_w8a8(*args, M, N, K, y.data_ptr(), ldy, code, _raw_stream()), "svdq_linear_w8a8")
     return y
 
 
-def _row_rho(rho, M, device):
-    """(the ratio of all rows, or a tensor of every row's)"""
+def _row_rho(rho, M, gpu):
+    """(the ratio of all rows, or the address of every row's)"""
     if not torch.is_tensor(rho):
         return float(rho), None
-    _need_tensor("rho", rho, torch.float32, (M,), device)
-    return 1.0, rho
+    return 1.0, _vector("rho", rho, _F32, (M,), gpu)
 
 
 def quantize_act_int8_grouped(x_bf16, offsets, inv_lambda=None, rho=1.0, rows=None, gelu=False, out=None):
     """quantize_act_int8 of rows in the experts' order: expert e owns rows offsets[e] .. offsets[e + 1] (int32 [E + 1]) and smooths them
     with inv_lambda[e] ([E,K]).  rows (int32 [M], any order, repeats allowed): row i is made of x[rows[i]]; None: of x[i].
     rho: a number or every row's ratio (f32 [M]).  Rows that no expert owns are not written."""
-    ldx = _need_rows("x", x_bf16, (torch.bfloat16,), (None, None))
-    (x_rows, K), device = x_bf16.shape, x_bf16.device
+    gpu = _gpu(x_bf16)
+    x_rows, K, ldx = _matrix("x", x_bf16, (_BF16,), gpu)
     M, E = (x_rows if rows is None else rows.numel()), offsets.numel() - 1
-    _need_tensor("offsets", offsets, torch.int32, (E + 1,), device)
-    if rows is not None:
-        _need_tensor("rows", rows, torch.int32, (M,), device)
-    if inv_lambda is not None:
-        _need_tensor("inv_lambda", inv_lambda, torch.float32, (E, K), device)
-    ratio, row_rho = _row_rho(rho, M, device)
-    qx, sx = _quantize_int8_out(out, M, K, device)
-    if M == 0:
-        return qx, sx
-    _check(load_library().svdq_quantize_act_int8_grouped(
-        _ptr(x_bf16), ldx, x_rows, _ptr(rows), _ptr(offsets), E, _ptr(inv_lambda), ratio, _ptr(row_rho), int(bool(gelu)), M, K,
-        _ptr(qx), _ptr(sx), _stream()), "svdq_quantize_act_int8_grouped")
+    o, r = _vector("offsets", offsets, _I32, (E + 1,), gpu), _optional("rows", rows, _I32, (M,), gpu)
+    il = _optional("inv_lambda", inv_lambda, _F32, (E, K), gpu)
+    ratio, row_rho = _row_rho(rho, M, gpu)
+    qx, sx = _quantize_int8_out(out, M, K, x_bf16, gpu)
+    if M:
+        _check((_lib or load_library()).svdq_quantize_act_int8_grouped(
+            x_bf16.data_ptr(), ldx, x_rows, r, o, E, il, ratio, row_rho, 1 if gelu else 0, M, K, qx.data_ptr(), sx.data_ptr(), _raw_stream()),
+            "svdq_quantize_act_int8_grouped")
     return qx, sx
 
 
 def linear_w8a8_grouped(qx, sx, offsets, qw, sw, bias=None, out=None, out_dtype=torch.bfloat16):
     """linear_w8a8 grouped by expert: rows offsets[e] .. offsets[e + 1] (int32 [E + 1]) of qx with qw[e] ([E,N,K] int8), sw[e] and bias[e]
     ([E,N] f32).  Rows that no expert owns are not written."""
-    _need_rows("qx", qx, (torch.int8,), (None, None))
-    _need(qx.is_contiguous(), "qx: a contiguous tensor is needed")
-    _need(qw.dim() == 3, "qw: [E, N, K] is needed")
-    (M, K), (E, N), device = qx.shape, qw.shape[:2], qx.device
-    _need_tensor("sx", sx, torch.float32, (M,), device)
-    _need_tensor("offsets", offsets, torch.int32, (E + 1,), device)
-    _need_tensor("qw", qw, torch.int8, (E, N, K), device)
-    _need_tensor("sw", sw, torch.float32, (E, N), device)
-    if bias is not None:
-        _need_tensor("bias", bias, torch.float32, (E, N), device)
-    y, ldy, code = _linear_out(out, M, N, out_dtype, device)
-    if M == 0:
-        return y
-    _check(load_library().svdq_linear_w8a8_grouped(_ptr(qx), _ptr(sx), _ptr(qw), _ptr(sw), _ptr(bias), _ptr(offsets), E, M, N, K,
-                                                   _ptr(y), ldy, code, _stream()), "svdq_linear_w8a8_grouped")
+    gpu = _gpu(qx)
+    if qx.dim() != 2 or qw.dim() != 3:
+        _refuse("qx, qw", qx if qx.dim() != 2 else qw, _I8, "[M, K], [E, N, K]", gpu)
+    (M, K), (E, N, _) = qx.shape, qw.shape
+    args = (_vector("qx", qx, _I8, (M, K), gpu), _vector("sx", sx, _F32, (M,), gpu), _vector("qw", qw, _I8, (E, N, K), gpu),
+            _vector("sw", sw, _F32, (E, N), gpu), _optional("bias", bias, _F32, (E, N), gpu), _vector("offsets", offsets, _I32, (E + 1,), gpu))
+    y, ldy, code = _linear_out(out, M, N, out_dtype, qx, gpu)
+    if M:
+        _check((_lib or load_library()).svdq_linear_w8a8_grouped(*args, E, M, N, K, y.data_ptr(), ldy, code, _raw_stream()), "svdq_linear_w8a8_grouped")
     return y
 
 
@@ -823,21 +836,18 @@ class _W8A8:
     def _descriptor(self):
         """svdq_layer_int8 of the tensors that the layer holds now, checked when they have changed.  The caller keeps it through
         its call."""
-        tensors = (self.inv_lambda, self.qw, self.sw, self.bias)
         held = self._held
-        if held is not None and all(a is b for a, b in zip(held[0], tensors)):
-            return held[1]
-        inv_lambda, qw, sw, bias = tensors
-        _need(qw.dim() == 2 + self.GROUPED, f"qw: {'[E, N, K]' if self.GROUPED else '[N, K]'} is needed, not {tuple(qw.shape)}")
-        lead, (N, K), device = tuple(qw.shape[:-2]), qw.shape[-2:], qw.device
-        _need_tensor("qw", qw, torch.int8, lead + (N, K), device)
-        _need_tensor("sw", sw, torch.float32, lead + (N,), device)
-        if inv_lambda is not None:
-            _need_tensor("inv_lambda", inv_lambda, torch.float32, lead + (K,), device)
-        if bias is not None:
-            _need_tensor("bias", bias, torch.float32, lead + (N,), device)
-        layer = _LayerInt8(lead[0] if lead else 0, N, K, _addr(inv_lambda), qw.data_ptr(), sw.data_ptr(), _addr(bias))
-        layer.address, layer.device = ctypes.addressof(layer), device
+        if held is not None:
+            a, b, c, d = held[0]
+            if a is self.inv_lambda and b is self.qw and c is self.sw and d is self.bias:
+                return held[1]
+        inv_lambda, qw, sw, bias = tensors = self.inv_lambda, self.qw, self.sw, self.bias
+        if qw.dim() != 2 + self.GROUPED:
+            raise ValueError(f"qw: {'[E, N, K]' if self.GROUPED else '[N, K]'} is needed, not {tuple(qw.shape)}")
+        lead, (N, K), gpu = tuple(qw.shape[:-2]), qw.shape[-2:], qw.get_device()
+        layer = _LayerInt8(lead[0] if lead else 0, N, K, _optional("inv_lambda", inv_lambda, _F32, lead + (K,), gpu), _vector("qw", qw, _I8, lead + (N, K), gpu),
+                           _vector("sw", sw, _F32, lead + (N,), gpu), _optional("bias", bias, _F32, lead + (N,), gpu))
+        layer.address, layer.shape = ctypes.addressof(layer), (layer.E, N, K, gpu)
         self._held = (tensors, layer)
         return layer
 
@@ -845,24 +855,21 @@ class _W8A8:
         """Copies make a descriptor of their own."""
         return {**self.__dict__, "_held": None}
 
-    def _forward(self, x, rows, offsets, rho, row_rho, gelu, M, out):
-        layer = self._descriptor()
-        ldx = _need_rows("x", x, (torch.bfloat16,), (None, layer.K))
-        device = x.device
-        _need(device == layer.device, f"x is on {device}, the layer on {layer.device}")
-        if out is None:
-            y, ldy = torch.empty((M, layer.N), dtype=torch.bfloat16, device=device), layer.N
-        else:
-            _need(out.dtype == torch.bfloat16, "out: bfloat16 is needed")
-            y, ldy, _ = _linear_out(out, M, layer.N, None, device)
-        if M == 0:
-            return y
-        # codes and scales of this call alone, from torch's allocator: calls on other streams and captured ones have their own
-        work = torch.empty(M * (layer.K + 4), dtype=torch.uint8, device=device)
-        codes = work.data_ptr()
-        _check((_lib or load_library()).svdq_layer_int8_forward(
-            layer.address, x.data_ptr(), ldx, x.shape[0], _addr(rows), _addr(offsets), rho, _addr(row_rho), 1 if gelu else 0, M,
-            codes, codes + M * layer.K, y.data_ptr(), ldy, _raw_stream()), "svdq_layer_int8_forward")
+    def _forward(self, x, layer, gpu, rows, offsets, rho, row_rho, gelu, M, out):
+        _, N, K, home = layer.shape
+        x_rows, _, ldx = _matrix("x", x, (_BF16,), gpu, K)
+        if home != gpu:
+            raise ValueError(f"x is on GPU {gpu}, the layer on {self.qw.device}")
+        y, ldy, code = _linear_out(out, M, N, _BF16, x, gpu)
+        if code != OUT_BF16:
+            _refuse("out", out, _BF16, (M, N), gpu)
+        if M:
+            # codes and scales of this call alone, from torch's allocator: calls on other streams and captured ones have their own
+            work = torch.empty(M * (K + 4), dtype=torch.uint8, device=x.device)
+            codes = work.data_ptr()
+            _check((_lib or load_library()).svdq_layer_int8_forward(
+                layer.address, x.data_ptr(), ldx, x_rows, rows, offsets, rho, row_rho, 1 if gelu else 0, M,
+                codes, codes + M * K, y.data_ptr(), ldy, _raw_stream()), "svdq_layer_int8_forward")
         return y
 
 
@@ -873,7 +880,7 @@ class W8A8Linear(_W8A8):
 
     def forward(self, x_bf16, rho=1.0, gelu=False, out=None):
         """x [M,K] bf16 -> y [M,N] bf16: quantize_act_int8 and linear_w8a8 in one call.  out may share memory with x."""
-        return self._forward(x_bf16, None, None, float(rho), None, gelu, x_bf16.shape[0], out)
+        return self._forward(x_bf16, self._descriptor(), _gpu(x_bf16), None, None, float(rho), None, gelu, x_bf16.shape[0], out)
 
 
 class W8A8Experts(_W8A8):
@@ -884,10 +891,8 @@ class W8A8Experts(_W8A8):
         """y [M,N] bf16 in the experts' order: rows offsets[e] .. offsets[e + 1] are expert e's, made of x[rows] (rows int32 [M]) or of x;
         rho a number or every row's ratio (f32 [M]).  quantize_act_int8_grouped and linear_w8a8_grouped in one call; rows that no
         expert owns are not written (without `out`: hold anything)."""
-        device = x_bf16.device
+        layer, gpu = self._descriptor(), _gpu(x_bf16)
         M = x_bf16.shape[0] if rows is None else rows.numel()
-        _need_tensor("offsets", offsets, torch.int32, (self.qw.shape[0] + 1,), device)
-        if rows is not None:
-            _need_tensor("rows", rows, torch.int32, (M,), device)
-        ratio, row_rho = _row_rho(rho, M, device)
-        return self._forward(x_bf16, rows, offsets, ratio, row_rho, gelu, M, out)
+        o, r = _vector("offsets", offsets, _I32, (layer.shape[0] + 1,), gpu), _optional("rows", rows, _I32, (M,), gpu)
+        ratio, row_rho = _row_rho(rho, M, gpu)
+        return self._forward(x_bf16, layer, gpu, r, o, ratio, row_rho, gelu, M, out)

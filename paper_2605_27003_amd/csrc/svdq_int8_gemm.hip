@@ -37,10 +37,11 @@ template <> struct Mfma<16> {
 // last channel, and every piece otherwise, goes element by element.
 template <class T, int I, int MT, int NT>
 struct TileStore {
-    static constexpr int EL = 16 / (int)sizeof(T), COLS = NT * I < 8 * EL ? NT * I : 8 * EL, ROWS = MT * I < 64 ? MT * I : 64;
+    static constexpr int EL = 16 / (int)sizeof(T), LINE = 8 * EL / I;  // blocks of a line
+    static constexpr int CB = NT % LINE == 0 ? LINE : NT % 2 == 0 && LINE > 2 ? 2 : 1, COLS = CB * I, ROWS = MT * I <= 64 ? MT * I : MT % (64 / I) == 0 ? 64 : 48;
     static constexpr int PITCH = COLS * (int)sizeof(T) + 16, BYTES = ROWS * PITCH;
-    static constexpr int CB = COLS / I, MP = ROWS / I, LANES = COLS / EL, STEP = 64 / LANES;
-    static_assert(NT % CB == 0 && MT % MP == 0 && ROWS % STEP == 0, "whole groups");
+    static constexpr int MP = ROWS / I, LANES = COLS / EL, STEP = 64 / LANES;
+    static_assert(NT % CB == 0 && MT % MP == 0, "whole groups");
     // region: BYTES of the wave's own.  tokens, channels, biases: LDS addresses of the wave's first.
     static __device__ __forceinline__ void run(const typename Mfma<I>::Acc (&acc)[NT][MT], const uint32_t region, const uint32_t tokens, const uint32_t channels, const uint32_t biases,
                                                const bool has_bias, const int lane, T* __restrict__ y, const int64_t ldy, const int rows, const int cols, const bool vec) {
@@ -80,8 +81,9 @@ struct TileStore {
                 const int r0 = lane / LANES, c = lane % LANES, left = cols - g * COLS;
                 T* const y0 = y + g * COLS + c * EL;
 #pragma unroll
-                for (int it = 0; it < ROWS / STEP; ++it) {
+                for (int it = 0; it < (ROWS + STEP - 1) / STEP; ++it) {
                     const int row = it * STEP + r0;
+                    if (ROWS % STEP && row >= ROWS) continue;
                     const uint4 v = lds_read16_pinned(region + row * PITCH + c * 16);
                     if (m0 * I + row >= rows) continue;
                     T* const p = y0 + (int64_t)(m0 * I + row) * ldy;
@@ -108,11 +110,11 @@ struct TileStore {
 template <int BM_, int BN_, int WM_, int WN_, int DEPTH_>
 struct Int8Tile {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, DEPTH = DEPTH_, I = 16, NW = WM * WN, THREADS = 64 * NW, MT = BM / WM / I, NT = BN / WN / I;
-    static constexpr int NA = BM / 8 / NW, NB = BN / 8 / NW;          // transfers of a wave a stage, eight rows each
+    static constexpr int NA = (BM / 8 + NW - 1) / NW, NB = (BN / 8 + NW - 1) / NW;                    // transfers of a wave a stage, eight rows each
     static constexpr uint32_t A = BM * BK, W = BN * BK, RING = (DEPTH + 1) * A + DEPTH * W;
     static constexpr int TOKENS = (BM + 63) / 64 * 64, CHANNELS = (BN + 63) / 64 * 64;                // scales and biases come 64 at a time
     static constexpr uint32_t SCALES = (TOKENS + 2 * CHANNELS) * 4;
-    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && DEPTH >= 2, "whole transfers");
+    static_assert(BM % (WM * I) == 0 && BN % (WN * I) == 0 && MT * NT % 2 == 0 && DEPTH >= 2, "whole blocks, and quarters of a stage's instructions");
 };
 
 // The tokens' rows of a stage, A(s), stand in a ring of DEPTH + 1 places, the channels', W(s), in one of DEPTH.  Stage s requests
@@ -135,11 +137,18 @@ void gemm_int8_kernel(const GemmInt8 g, const TileGrid tg) {
     const int K = g.K, N = g.N;
     const uint32_t ring_a = (uint32_t)(uintptr_t)(lds_byte*)ring, ring_w = ring_a + (DEPTH + 1) * G::A;
     TilePlace at;
-    if (!tile_place<BM, BN, GROUPED>(g, tg, blockIdx.x, lane, at)) return;
+    if constexpr (GROUPED) {
+        if (!tile_place<BM, BN>(g, tg, GroupScan(g.groups, (int)g.M, BM, lane), blockIdx.x, at)) return;
+    } else {
+        if (!tile_place<BM, BN>(g, tg, blockIdx.x, at)) return;
+    }
     const int m0 = at.m0, m_end = at.m_end, n0 = at.n0;
     const int nstages = (K + BK - 1) / BK;
 
-    // ---- transfers: j of this wave covers rows 8 (wave NA + j) .. + 7
+    // ---- transfers: j of this wave covers rows 8 (wave NA + j) .. + 7 (where that is past the tile: its last eight rows again)
+    const int a0 = wave * NA, w0 = wave * NB;
+    auto block_a = [&](const int j) { return BM / 8 % G::NW == 0 || a0 + j < BM / 8 ? a0 + j : BM / 8 - 1; };
+    auto block_w = [&](const int j) { return BN / 8 % G::NW == 0 || w0 + j < BN / 8 ? w0 + j : BN / 8 - 1; };
     const int8_t* const abase = g.qx + (int64_t)m0 * K;
     const int8_t* const wbase = at.qw + (int64_t)n0 * K;
     const int place = lane & 7;
@@ -150,9 +159,9 @@ void gemm_int8_kernel(const GemmInt8 g, const TileGrid tg) {
         v = (uint32_t)(row < last ? row : last) * (uint32_t)K + piece * 16;
     };
 #pragma unroll
-    for (int j = 0; j < NA; ++j) rows_of(va[j], pa[j], wave * NA + j, m_end - 1 - m0);
+    for (int j = 0; j < NA; ++j) rows_of(va[j], pa[j], block_a(j), m_end - 1 - m0);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) rows_of(vw[j], pw[j], wave * NB + j, N - 1 - n0);
+    for (int j = 0; j < NB; ++j) rows_of(vw[j], pw[j], block_w(j), N - 1 - n0);
     auto request = [&](const int8_t* base, uint32_t v, const uint32_t piece, const int s, const uint32_t to) {
         if constexpr (TAIL) {
             const int left = (K >> 4) - 8 * s - 1, over = (int)piece - left;
@@ -160,8 +169,8 @@ void gemm_int8_kernel(const GemmInt8 g, const TileGrid tg) {
         }
         dma16(base + (int64_t)s * BK, v, to);
     };
-    auto request_a = [&](const int s, const uint32_t to, const int j) { request(abase, va[j], pa[j], s, to + (wave * NA + j) * 1024); };
-    auto request_w = [&](const int s, const uint32_t to, const int j) { request(wbase, vw[j], pw[j], s, to + (wave * NB + j) * 1024); };
+    auto request_a = [&](const int s, const uint32_t to, const int j) { request(abase, va[j], pa[j], s, to + block_a(j) * 1024); };
+    auto request_w = [&](const int s, const uint32_t to, const int j) { request(wbase, vw[j], pw[j], s, to + block_w(j) * 1024); };
     auto next_a = [&](const uint32_t c) { return c == ring_a + DEPTH * G::A ? ring_a : c + G::A; };
     auto next_w = [&](const uint32_t c) { return c == ring_w + (DEPTH - 1) * G::W ? ring_w : c + G::W; };
 
