@@ -6,23 +6,18 @@
 // registers.  (Operands straight to registers would be sixteen rows' pieces a load: 38 bytes a ns a CU from L2 where transfers of
 // whole lines, eight lanes a row, reach 135.)  Blocks walk the tiles: a wave's requests run on into its next tiles while sums are added up and
 // stored, since with a short K a tile is little more than its start.  The partial sums, exact integers in any order, meet in LDS.
-#include <type_traits>
-
 #include "svdq_int8_dev.h"
+#include "svdq_int8_plan.h"
 
 namespace svdq {
 
 namespace {
 
-constexpr int CUS = 8 * CUS_PER_XCD;
-
-struct NoScan {
-    static constexpr int total = 0;
-};
+constexpr int CUS = 256;
 
 template <int TOK, int BN, int NW, int DEPTH, bool TAIL, bool GROUPED, class T>
 __global__ __launch_bounds__(64 * NW)
-void gemm_int8_few_kernel(const GemmInt8 g, const TileGrid tg, const int walkers) {
+void gemm_int8_few_kernel(const GemmInt8 g, const int walkers) {
     constexpr int TT = TOK / 16, CT = BN / 16, NA = TOK / 8, NB = BN / 8, ND = NA + NB, OUT = (TOK * BN + 64 * NW - 1) / (64 * NW), ROWS = 64 * NW / BN;
     constexpr uint32_t STAGE = (TOK + BN) * BK, SUMS = CT * TT * 64 * 16, SCALES = 3 * 256;
     // rings; then every wave's sums; then the scales and biases of a tile, of the DEPTH that requests can be ahead, and of the one before, which
@@ -38,21 +33,7 @@ void gemm_int8_few_kernel(const GemmInt8 g, const TileGrid tg, const int walkers
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte*)lds, mine = lds0 + wave * DEPTH * STAGE;
     const int nstages = (K + BK - 1) / BK, count = (nstages - wave + NW - 1) / NW;       // a tile's stages of this wave
 
-    const std::conditional_t<GROUPED, GroupScan, NoScan> scan = [&] {
-        if constexpr (GROUPED) return GroupScan(g.groups, (int)g.M, TOK, lane);
-        else return NoScan{};
-    }();
-    const int ids = GROUPED ? (scan.total * tg.ntiles + 7) / 8 * 8 : tile_ids(tg);
-    // the first tile from `id` on, in steps of `walkers`
-    auto find = [&](int& id, TilePlace& p) {
-        for (; id < ids; id += walkers) {
-            bool is;
-            if constexpr (GROUPED) is = tile_place<TOK, BN>(g, tg, scan, id, p);
-            else is = tile_place<TOK, BN>(g, tg, id, p);
-            if (is) return true;
-        }
-        return false;
-    };
+    const typename TilesOf<GROUPED, TOK, BN>::type tiles(g, lane);
 
     // ---- requests: eight rows each, the tokens' first; rows past the end repeat the last one.  Ahead of a tile's first, wave 0 asks for its scales.
     int rid = blockIdx.x, rstage = 0, rtile = 0;                      // what is requested next
@@ -63,7 +44,7 @@ void gemm_int8_few_kernel(const GemmInt8 g, const TileGrid tg, const int walkers
     auto request = [&] {
         if (rstage == 0) {
             TilePlace p;
-            more = more && find(rid, p);
+            more = more && tiles.place(g, rid, p);                    // (where a block has no tile it has none behind it)
             if (!more) return;
             const int rows = p.m_end - p.m0, cols = N - p.n0;
             abase = g.qx + (int64_t)p.m0 * K;
@@ -111,7 +92,7 @@ void gemm_int8_few_kernel(const GemmInt8 g, const TileGrid tg, const int walkers
     typedef const volatile __attribute__((address_space(3))) int4v lds_i4;
     TilePlace p;
     int tile = 0;
-    for (int id = blockIdx.x; find(id, p); id += walkers) {
+    for (int id = blockIdx.x; tiles.place(g, id, p); id += walkers) {
         int4v acc[CT][TT];
 #pragma unroll
         for (int c = 0; c < CT; ++c)
@@ -183,11 +164,9 @@ void gemm_int8_few_kernel(const GemmInt8 g, const TileGrid tg, const int walkers
 
 template <int TOK, int BN, int NW, int DEPTH>
 hipError_t launch(const GemmInt8& g, const bool out_f32, hipStream_t stream) {
-    const int ntiles = (g.N + BN - 1) / BN;
     const bool grouped = g.groups.offsets != nullptr;
-    const TileGrid tg = grouped ? TileGrid{0, ntiles, 0, 0} : make_tile_grid((int)((g.M + TOK - 1) / TOK), ntiles);
-    const int most = grouped ? grouped_blocks(g, TOK, BN) : tile_ids(tg), walkers = most < 2 * CUS ? most : 2 * CUS;
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(walkers), dim3(64 * NW), 0, stream, g, tg, walkers); };
+    const int most = most_tiles(g, TOK, BN), walkers = most < 2 * CUS ? most : 2 * CUS;  // multiples of 256, as tile_number asks
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(walkers), dim3(64 * NW), 0, stream, g, walkers); };
     auto typed = [&](auto TAILC, auto GROUPEDC) {
         constexpr bool TAIL = decltype(TAILC)::value, GROUPED = decltype(GROUPEDC)::value;
         if (out_f32) go(gemm_int8_few_kernel<TOK, BN, NW, DEPTH, TAIL, GROUPED, uint32_t>);
@@ -200,12 +179,17 @@ hipError_t launch(const GemmInt8& g, const bool out_f32, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_gemm_int8_few(const GemmInt8& g, const int tokens, bool out_f32, hipStream_t stream) {
-    // Thirty-two channels a block where that makes enough blocks (half the tokens' transfers of sixteen: 24 tokens, 5120 x 5120 7.8
-    // against 9.2 us); otherwise sixteen, and eight waves (one token, N = 1024, K = 13824: 5.6 against 7.4 us).
-    const bool wide = g.N >= 4096 || g.groups.offsets;
-    if (tokens <= 16) return wide ? launch<16, 32, 4, 2>(g, out_f32, stream) : launch<16, 16, 8, 2>(g, out_f32, stream);
-    return wide ? launch<32, 32, 4, 2>(g, out_f32, stream) : launch<32, 16, 8, 2>(g, out_f32, stream);
+// Thirty-two channels a block halve the tokens' transfers (24 tokens, 5120 x 5120: 7.8 against 9.2 us); sixteen, on eight waves, where there
+// are few blocks (one token, N = 1024, K = 13824: 5.6 against 7.4 us).
+hipError_t launch_gemm_int8_few(const GemmInt8& g, const Int8Plan& p, bool out_f32, hipStream_t stream) {
+    switch (p.tiles) {
+        case Int8Tiles::FEW_16x16: return launch<16, 16, 8, 2>(g, out_f32, stream);
+        case Int8Tiles::FEW_16x32:                                    // one round of blocks: a stage more in flight (6.9 against 7.8 us at N = K = 5120)
+            if (!g.groups.offsets && g.M <= 16 && g.N <= 32 * CUS) return launch<16, 32, 4, 3>(g, out_f32, stream);
+            return launch<16, 32, 4, 2>(g, out_f32, stream);
+        case Int8Tiles::FEW_32x16: return launch<32, 16, 8, 2>(g, out_f32, stream);
+        default: return launch<32, 32, 4, 2>(g, out_f32, stream);
+    }
 }
 
 }  // namespace svdq

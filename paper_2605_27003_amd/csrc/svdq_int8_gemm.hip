@@ -10,8 +10,7 @@
 // lanes pick their pieces in rotated order: piece c of row r stands at place c ^ ((r / 2) % 8) of its 128 bytes.  The 32 rows
 // that an operand read covers then meet all banks evenly.
 #include "svdq_int8_dev.h"
-#include "svdq_kernels.h"
-#include "svdq_tiles.h"
+#include "svdq_int8_plan.h"
 
 namespace svdq {
 
@@ -32,19 +31,19 @@ template <> struct Mfma<16> {
 };
 
 // The end of a tile whose scales and biases stand in LDS (binary32: the tokens', the channels', the channels' biases): y = acc sx sw + bias,
-// up to 64 tokens at a time in column groups whose rows are one memory line (128 bytes) where the wave has as many channels, each
-// transposed through the wave's own LDS and stored 16 bytes a lane.  `vec`: whole pieces can be stored as 16 bytes; a piece over the
-// last channel, and every piece otherwise, goes element by element.
-template <class T, int I, int MT, int NT>
+// up to MOST tokens at a time in column groups whose rows are one memory line (128 bytes) where the wave has as many channels, each
+// transposed through the wave's own LDS and stored `unit` bytes a lane, as the rows' alignment allows: 16 (a piece over the last channel goes
+// element by element), 4, or an element.
+template <class T, int I, int MT, int NT, int MOST>
 struct TileStore {
     static constexpr int EL = 16 / (int)sizeof(T), LINE = 8 * EL / I;  // blocks of a line
-    static constexpr int CB = NT % LINE == 0 ? LINE : NT % 2 == 0 && LINE > 2 ? 2 : 1, COLS = CB * I, ROWS = MT * I <= 64 ? MT * I : MT % (64 / I) == 0 ? 64 : 48;
+    static constexpr int CB = NT % LINE == 0 ? LINE : NT % 2 == 0 && LINE > 2 ? 2 : 1, COLS = CB * I, ROWS = MT * I <= MOST ? MT * I : MOST;
     static constexpr int PITCH = COLS * (int)sizeof(T) + 16, BYTES = ROWS * PITCH;
     static constexpr int MP = ROWS / I, LANES = COLS / EL, STEP = 64 / LANES;
     static_assert(NT % CB == 0 && MT % MP == 0, "whole groups");
     // region: BYTES of the wave's own.  tokens, channels, biases: LDS addresses of the wave's first.
     static __device__ __forceinline__ void run(const typename Mfma<I>::Acc (&acc)[NT][MT], const uint32_t region, const uint32_t tokens, const uint32_t channels, const uint32_t biases,
-                                               const bool has_bias, const int lane, T* __restrict__ y, const int64_t ldy, const int rows, const int cols, const bool vec) {
+                                               const bool has_bias, const int lane, T* __restrict__ y, const int64_t ldy, const int rows, const int cols, const int unit) {
         const int li = lane % I, lk = lane / I;
 #pragma unroll
         for (int m0 = 0; m0 < MT; m0 += MP) {
@@ -78,25 +77,47 @@ struct TileStore {
                     }
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
                 __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-                const int r0 = lane / LANES, c = lane % LANES, left = cols - g * COLS;
-                T* const y0 = y + g * COLS + c * EL;
+                const int left = cols - g * COLS;
+                T* const y0 = y + g * COLS;
+                if (unit == 16) {
+                    const int r0 = lane / LANES, c = lane % LANES;
 #pragma unroll
-                for (int it = 0; it < (ROWS + STEP - 1) / STEP; ++it) {
-                    const int row = it * STEP + r0;
-                    if (ROWS % STEP && row >= ROWS) continue;
-                    const uint4 v = lds_read16_pinned(region + row * PITCH + c * 16);
-                    if (m0 * I + row >= rows) continue;
-                    T* const p = y0 + (int64_t)(m0 * I + row) * ldy;
-                    if (vec && (c + 1) * EL <= left) {
-                        *reinterpret_cast<uint4*>(p) = v;
-                    } else {
-                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                    for (int it = 0; it < (ROWS + STEP - 1) / STEP; ++it) {
+                        const int row = it * STEP + r0;
+                        if (ROWS % STEP && row >= ROWS) continue;
+                        const uint4 v = lds_read16_pinned(region + row * PITCH + c * 16);
+                        if (m0 * I + row >= rows) continue;
+                        T* const p = y0 + (int64_t)(m0 * I + row) * ldy + c * EL;
+                        if ((c + 1) * EL <= left) {
+                            *reinterpret_cast<uint4*>(p) = v;
+                        } else {
+                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                        for (int i = 0; i < EL; ++i)
-                            if (c * EL + i < left) {
-                                if constexpr (sizeof(T) == 2) p[i] = (T)(w[i >> 1] >> (16 * (i & 1)));
-                                else p[i] = w[i];
-                            }
+                            for (int i = 0; i < EL; ++i)
+                                if (c * EL + i < left) {
+                                    if constexpr (sizeof(T) == 2) p[i] = (T)(w[i >> 1] >> (16 * (i & 1)));
+                                    else p[i] = w[i];
+                                }
+                        }
+                    }
+                } else {
+                    // four bytes a lane, or two: consecutive lanes store consecutive elements
+                    constexpr int WORDS = COLS * (int)sizeof(T) / 4;
+                    const int n = ROWS * WORDS * (unit == 4 ? 1 : 2), per = WORDS * (unit == 4 ? 1 : 2);
+                    for (int i = lane; i < n; i += 64) {
+                        const int row = i / per, c = i - row * per;
+                        if (m0 * I + row >= rows) break;
+                        T* const p = y0 + (int64_t)(m0 * I + row) * ldy;
+                        const uint32_t v = lds_read4(region + row * PITCH + (unit == 4 ? c : c >> 1) * 4);
+                        if constexpr (sizeof(T) == 4) {
+                            if (c < left) p[c] = v;
+                        } else if (unit == 4 && 2 * c + 1 < left) {
+                            *reinterpret_cast<uint32_t*>(p + 2 * c) = v;
+                        } else if (unit == 4) {
+                            if (2 * c < left) p[2 * c] = (T)v;
+                        } else if (c < left) {
+                            p[c] = (T)(v >> (16 * (c & 1)));
+                        }
                     }
                 }
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -123,10 +144,10 @@ struct Int8Tile {
 // (with a place less and all of them there, 256 x 256 tiles took 6 % longer at K = 13824).
 template <class G, bool TAIL, bool GROUPED, class T>
 __global__ __launch_bounds__(G::THREADS, 1)
-void gemm_int8_kernel(const GemmInt8 g, const TileGrid tg) {
+void gemm_int8_kernel(const GemmInt8 g) {
     constexpr int BM = G::BM, BN = G::BN, MT = G::MT, NT = G::NT, NA = G::NA, NB = G::NB, I = G::I, DEPTH = G::DEPTH;
     using Acc = typename Mfma<I>::Acc;
-    using Store = TileStore<T, I, MT, NT>;
+    using Store = TileStore<T, I, MT, NT, (G::RING >= (G::NW + 1) * 64 * 144 + G::SCALES ? 64 : 32)>;
     static_assert(G::RING >= (G::NW + 1) * Store::BYTES + G::SCALES && G::A >= G::SCALES, "the store transposes in the ring, beside the scales");
     __shared__ __attribute__((aligned(16))) uint8_t ring[G::RING];
 
@@ -137,11 +158,7 @@ void gemm_int8_kernel(const GemmInt8 g, const TileGrid tg) {
     const int K = g.K, N = g.N;
     const uint32_t ring_a = (uint32_t)(uintptr_t)(lds_byte*)ring, ring_w = ring_a + (DEPTH + 1) * G::A;
     TilePlace at;
-    if constexpr (GROUPED) {
-        if (!tile_place<BM, BN>(g, tg, GroupScan(g.groups, (int)g.M, BM, lane), blockIdx.x, at)) return;
-    } else {
-        if (!tile_place<BM, BN>(g, tg, blockIdx.x, at)) return;
-    }
+    if (!typename TilesOf<GROUPED, BM, BN>::type(g, lane).place(g, blockIdx.x, at)) return;
     const int m0 = at.m0, m_end = at.m_end, n0 = at.n0;
     const int nstages = (K + BK - 1) / BK;
 
@@ -283,65 +300,47 @@ void gemm_int8_kernel(const GemmInt8 g, const TileGrid tg) {
     }
     stage(s, IC<0>{}, IC<1>{});
 
-    const bool vec = ((reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)(g.ldy * (int64_t)sizeof(T))) & 15) == 0;
+    const uintptr_t ends = reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)(g.ldy * (int64_t)sizeof(T));
+    const int unit = (ends & 15) == 0 ? 16 : (ends & 3) == 0 ? 4 : 2;
     const int mw = m0 + wm * MT * I, nw = n0 + wn * NT * I;
     if (nw >= N || mw >= m_end) return;
     const int below = (int)(scales - ring_a) / Store::BYTES;          // waves whose store area fits below the scales
     const uint32_t region = wave < below ? ring_a + wave * Store::BYTES : scales + G::SCALES + (wave - below) * Store::BYTES;
     Store::run(acc, region, scales + wm * MT * I * 4, scales + (G::TOKENS + wn * NT * I) * 4, scales + (G::TOKENS + G::CHANNELS + wn * NT * I) * 4,
-               at.bias != nullptr, lane, reinterpret_cast<T*>(g.y) + (int64_t)mw * g.ldy + nw, g.ldy, m_end - mw, N - nw, vec);
-}
-
-template <class G, bool TAIL, bool GROUPED>
-void launch_tiles_t(const GemmInt8& g, const bool out_f32, const TileGrid& tg, const int blocks, hipStream_t stream) {
-    if (out_f32) hipLaunchKernelGGL((gemm_int8_kernel<G, TAIL, GROUPED, uint32_t>), dim3(blocks), dim3(G::THREADS), 0, stream, g, tg);
-    else hipLaunchKernelGGL((gemm_int8_kernel<G, TAIL, GROUPED, uint16_t>), dim3(blocks), dim3(G::THREADS), 0, stream, g, tg);
+               at.bias != nullptr, lane, reinterpret_cast<T*>(g.y) + (int64_t)mw * g.ldy + nw, g.ldy, m_end - mw, N - nw, unit);
 }
 
 template <class G>
 hipError_t launch_tiles(const GemmInt8& g, const bool out_f32, hipStream_t stream) {
-    const int ntiles = (g.N + G::BN - 1) / G::BN;
-    const bool tail = g.K % BK != 0;
-    if (g.groups.offsets) {
-        const int blocks = (int)grouped_blocks(g, G::BM, G::BN);
-        const TileGrid tg{0, ntiles, 0, 0};
-        if (tail) launch_tiles_t<G, true, true>(g, out_f32, tg, blocks, stream);
-        else launch_tiles_t<G, false, true>(g, out_f32, tg, blocks, stream);
-        return hipGetLastError();
-    }
-    const TileGrid tg = make_tile_grid((int)((g.M + G::BM - 1) / G::BM), ntiles);
-    if (tail) launch_tiles_t<G, true, false>(g, out_f32, tg, tile_ids(tg), stream);
-    else launch_tiles_t<G, false, false>(g, out_f32, tg, tile_ids(tg), stream);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(most_tiles(g, G::BM, G::BN)), dim3(G::THREADS), 0, stream, g); };
+    auto typed = [&](auto TAILC, auto GROUPEDC) {
+        constexpr bool TAIL = decltype(TAILC)::value, GROUPED = decltype(GROUPEDC)::value;
+        if (out_f32) go(gemm_int8_kernel<G, TAIL, GROUPED, uint32_t>);
+        else go(gemm_int8_kernel<G, TAIL, GROUPED, uint16_t>);
+    };
+    const bool grouped = g.groups.offsets != nullptr;
+    if (g.K % BK) grouped ? typed(IC<1>{}, IC<1>{}) : typed(IC<1>{}, IC<0>{});
+    else grouped ? typed(IC<0>{}, IC<1>{}) : typed(IC<0>{}, IC<0>{});
     return hipGetLastError();
 }
 
-using T256 = Int8Tile<256, 256, 2, 4, 2>;
-using T128 = Int8Tile<128, 128, 2, 4, 4>;
-using T64 = Int8Tile<64, 64, 2, 2, 4>;
-
 }  // namespace
 
-// Tiles are chosen by the rows that there are (an expert, on average).
-enum class Int8Plan { FEW, T64, T128, T256 };
-static Int8Plan plan(const GemmInt8& g) {
-    const int64_t rows = g.groups.offsets ? (g.M + g.groups.E - 1) / g.groups.E : g.M;
-    return rows <= 64 ? Int8Plan::FEW : rows <= 256 ? Int8Plan::T64 : rows <= 1024 ? Int8Plan::T128 : Int8Plan::T256;
-}
-
-// Block ids and tile numbers are 32-bit.
-bool gemm_int8_fits(const GemmInt8& g) {
-    const Int8Plan p = plan(g);
-    const int bm = p == Int8Plan::T256 ? 256 : p == Int8Plan::T128 ? 128 : p == Int8Plan::T64 ? 64 : 16, bn = bm;
-    const int64_t mt = (g.M + bm - 1) / bm + (g.groups.offsets ? g.groups.E : 0), nt = ((int64_t)g.N + bn - 1) / bn;
-    return (mt + 8) * (nt + 8) < INT32_MAX;
-}
+bool gemm_int8_fits(const GemmInt8& g) { return g.M == 0 || int8_plan(g.M, g.N, g.K, g.groups.offsets ? g.groups.E : 0, false).cost >= 0.0; }
 
 hipError_t launch_gemm_int8(const GemmInt8& g, bool out_f32, hipStream_t stream) {
-    switch (plan(g)) {
-        case Int8Plan::FEW: return launch_gemm_int8_few(g, (int)(g.groups.offsets ? (g.M + g.groups.E - 1) / g.groups.E : g.M), out_f32, stream);
-        case Int8Plan::T64: return launch_tiles<T64>(g, out_f32, stream);
-        case Int8Plan::T128: return launch_tiles<T128>(g, out_f32, stream);
-        default: return launch_tiles<T256>(g, out_f32, stream);
+    const Int8Plan p = int8_plan(g.M, g.N, g.K, g.groups.offsets ? g.groups.E : 0, out_f32);
+    switch (p.tiles) {
+        case Int8Tiles::T64x32: return launch_tiles<Int8Tile<64, 32, 2, 2, 4>>(g, out_f32, stream);
+        case Int8Tiles::T64x64: return launch_tiles<Int8Tile<64, 64, 2, 2, 4>>(g, out_f32, stream);
+        case Int8Tiles::T64x128: return launch_tiles<Int8Tile<64, 128, 2, 4, 3>>(g, out_f32, stream);
+        case Int8Tiles::T128x128:                                     // a block alone on its CU, or two
+            if (most_tiles(g, 128, 128) <= 256) return launch_tiles<Int8Tile<128, 128, 2, 4, 4>>(g, out_f32, stream);
+            return launch_tiles<Int8Tile<128, 128, 2, 4, 2>>(g, out_f32, stream);
+        case Int8Tiles::T256x128: return launch_tiles<Int8Tile<256, 128, 4, 2, 2>>(g, out_f32, stream);
+        case Int8Tiles::T256x160: return launch_tiles<Int8Tile<256, 160, 4, 2, 2>>(g, out_f32, stream);
+        case Int8Tiles::T256x256: return launch_tiles<Int8Tile<256, 256, 2, 4, 2>>(g, out_f32, stream);
+        default: return launch_gemm_int8_few(g, p, out_f32, stream);
     }
 }
 

@@ -1,0 +1,84 @@
+// Which tiles a product of the 8-bit layer takes, and in which order (host only).  All give the same sums, exact integers.
+#pragma once
+#include <cstdint>
+
+namespace svdq {
+
+enum class Int8Tiles { FEW_16x16, FEW_16x32, FEW_32x16, FEW_32x32, T64x32, T64x64, T64x128, T128x128, T256x128, T256x160, T256x256 };
+constexpr int INT8_TILES = 11;
+struct Int8TileShape {
+    int bm, bn;
+    double stage;                // us of a block alone on its CU for 128 k; 0: the few-token kernel
+    int per_cu;                  // blocks that fit a CU's LDS
+};
+// A block's time goes by the bytes that it brings to LDS, about 75 a ns where some come from its XCD's L2 and some from behind it (135 where all
+// come from L2, 50 where none do), whatever is in flight; 256 x 256 comes near the matrix pipes' time.  Measured at K = 5120 with one
+// round of blocks, one per CU.
+inline Int8TileShape int8_tile_shape(Int8Tiles t) {
+    switch (t) {
+        case Int8Tiles::FEW_16x16: return {16, 16, 0.0, 2};
+        case Int8Tiles::FEW_16x32: return {16, 32, 0.0, 2};
+        case Int8Tiles::FEW_32x16: return {32, 16, 0.0, 1};
+        case Int8Tiles::FEW_32x32: return {32, 32, 0.0, 1};
+        case Int8Tiles::T64x32: return {64, 32, 0.17, 2};
+        case Int8Tiles::T64x64: return {64, 64, 0.21, 2};
+        case Int8Tiles::T64x128: return {64, 128, 0.31, 2};
+        case Int8Tiles::T128x128: return {128, 128, 0.415, 2};
+        case Int8Tiles::T256x128: return {256, 128, 0.62, 1};
+        case Int8Tiles::T256x160: return {256, 160, 0.73, 1};
+        default: return {256, 256, 1.07, 1};
+    }
+}
+
+struct Int8Plan {
+    Int8Tiles tiles;
+    double cost;                 // estimate, us; negative: the tiles cannot be numbered in 32 bits
+};
+
+// rows: of the call.  experts: 0 where it is not grouped.
+// Estimate for one choice: a launch and its first bytes 2.5, and the longest of
+//   rounds     a block's stages and its end, for as many rounds as there are tiles for each of 256 CUs (two blocks that share a CU take 1.75 times as
+//              long as one)
+//   fabric     what the XCDs' L2s fetch at 6 TB/s: 256 tiles at a time, each XCD the rows and channels of its share of them
+//   memory     weights, codes and outputs at 5.5 TB/s
+// and a little of the first two, which decides where choices share their bound.
+inline Int8Plan int8_cost(Int8Tiles t, int64_t rows, int N, int K, int experts, bool out_f32) {
+    const Int8TileShape s = int8_tile_shape(t);
+    const int64_t with_rows = experts ? (rows < experts ? rows : experts) : 1, nt = ((int64_t)N + s.bn - 1) / s.bn;
+    const int64_t most = experts ? rows / s.bm + with_rows : (rows + s.bm - 1) / s.bm;                // row tiles that there can be
+    const double mt = experts ? (double)rows / s.bm + 0.5 * with_rows : (double)most;                 // and that there are, on average
+    Int8Plan p{t, -1.0};
+    if ((most + 8) * (nt + 8) + 512 >= INT32_MAX) return p;
+    const double weights = (double)with_rows * N * K, codes = (double)rows * K, tiles = mt * nt;
+    const double across = mt / with_rows < 8 ? (mt / with_rows < 1 ? 1 : mt / with_rows) : 8, share = tiles < 256 ? tiles / 8 : 32;    // an XCD's tiles: row tiles, all
+    const double shared = share / across < 1 ? share : across, channels = share / across < 1 ? 1 : share / across;
+    double fabric = tiles / share * (shared * s.bm + channels * s.bn) * K;
+    if (fabric < weights + codes) fabric = weights + codes;
+    const double memory = weights + codes + (double)rows * N * (out_f32 ? 4 : 2);
+    // rounds of blocks, in the time of one block alone on its CU
+    const double n = tiles / 256.0, whole = experts ? n + 0.3 : (double)(int64_t)(n + 0.999);
+    const double rounds = n <= 1.0 ? 1.0 : s.per_cu == 2 ? (n <= 2.0 ? 1.75 : 0.92 * n) : whole;
+    double time;
+    if (s.stage == 0.0) {
+        const double used = experts ? (rows < 2 * experts ? 2.0 : (double)s.bm) : (double)(rows < s.bm ? rows : s.bm);      // rows past the last are in L1 already
+        time = (s.per_cu == 2 && n > 1.0 ? n : rounds) * ((used + s.bn) * K / 50.0e3 + 0.4);   // walking blocks share their CU evenly
+    } else {
+        time = rounds * (((K + 127) / 128) * s.stage + 0.6 + 4.3 * s.bm * s.bn / 65536.0);
+    }
+    double most_time = time;
+    if (fabric / 6.0e6 > most_time) most_time = fabric / 6.0e6;
+    if (memory / 5.5e6 > most_time) most_time = memory / 5.5e6;
+    p.cost = 2.5 + most_time + 0.15 * (time + fabric / 6.0e6);        // the others matter where two choices share their bound
+    return p;
+}
+
+inline Int8Plan int8_plan(int64_t rows, int N, int K, int experts, bool out_f32) {
+    Int8Plan best{Int8Tiles::T256x256, -1.0};
+    for (int i = 0; i < INT8_TILES; ++i) {
+        const Int8Plan p = int8_cost((Int8Tiles)i, rows, N, K, experts, out_f32);
+        if (p.cost >= 0.0 && (best.cost < 0.0 || p.cost < 0.995 * best.cost)) best = p;
+    }
+    return best;
+}
+
+}  // namespace svdq

@@ -35,13 +35,17 @@ void quantize_int8_kernel(const QuantInt8 q, const int run) {
     }
     const int64_t begin = ((int64_t)blockIdx.x * TEAMS + team) * run;
     const uint16_t* const x = reinterpret_cast<const uint16_t*>(q.x);
+    // the run's rows of x and ratios, a lane each
+    const int64_t ahead = begin + lane < q.M ? begin + lane : q.M - 1;
+    const int tokens = q.rows ? q.rows[ahead] : 0;
+    const float ratios = q.row_rho ? q.row_rho[ahead] : q.rho;
 
-    auto load = [&](uint4 (&v)[C], const int64_t row) {
-        int64_t r = row;
-        bool none = row >= q.M;
-        if (!none && q.rows) {
-            r = q.rows[row];
-            none = r < 0 || r >= q.x_rows;                           // no such token: zeros
+    auto load = [&](uint4 (&v)[C], const int i) {                    // the run's i-th row
+        int64_t r = begin + i;
+        bool none = r >= q.M;
+        if (q.rows) {
+            r = __builtin_amdgcn_readlane(tokens, i);
+            none = none || r < 0 || r >= q.x_rows;                   // no such token: zeros
         }
         if (none) {
 #pragma unroll
@@ -63,8 +67,13 @@ void quantize_int8_kernel(const QuantInt8 q, const int run) {
         }
     };
     uint4 next[C];
-    load(next, begin);
-    int expert = -1;
+    load(next, 0);
+    // number of the first offset past the row: it only grows along the run
+    int expert = -1, past = 0, past_offset = 0;
+    if constexpr (GROUPED) {
+        past = first_offset_past(q.groups, begin, lane);
+        past_offset = past <= q.groups.E ? q.groups.offsets[past] : 0;
+    }
     if (!GROUPED && q.inv_lambda) load_il(0);
 
     for (int i = 0; i < run; ++i) {
@@ -73,15 +82,15 @@ void quantize_int8_kernel(const QuantInt8 q, const int run) {
         uint4 v[C];
 #pragma unroll
         for (int c = 0; c < C; ++c) v[c] = next[c];
-        if (i + 1 < run) load(next, row + 1);
+        if (i + 1 < run) load(next, i + 1);
         bool owned = row < q.M;
         if constexpr (GROUPED) {
-            if (owned) {
-                const int e = expert_of_row(q.groups, row, lane);
-                owned = e >= 0;
-                if (owned && e != expert && q.inv_lambda) load_il(e);
-                if (owned) expert = e;
-            }
+            while (past <= q.groups.E && past_offset <= row)
+                if (++past <= q.groups.E) past_offset = q.groups.offsets[past];
+            const int e = past - 1;
+            owned = owned && e >= 0 && past <= q.groups.E;
+            if (owned && e != expert && q.inv_lambda) load_il(e);
+            if (owned) expert = e;
         }
         float xs[C][8];
         uint32_t top = 0;
@@ -119,7 +128,7 @@ void quantize_int8_kernel(const QuantInt8 q, const int run) {
         }
         if (!owned) continue;
         const bool finite = top < 0x7f800000u;
-        const float rho = q.row_rho ? q.row_rho[row] : q.rho;
+        const float rho = bits_f((uint32_t)__builtin_amdgcn_readlane((int)f_bits(ratios), i));
         float s = __fdiv_rn(__fmul_rn(rho, bits_f(top)), QMAX8);
         const bool fine = finite && s >= 1.17549435e-38f;
         const float inv = fine ? __fdiv_rn(1.0f, s) : 0.0f;
