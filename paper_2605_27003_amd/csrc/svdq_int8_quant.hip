@@ -15,12 +15,22 @@ namespace svdq {
 
 namespace {
 
-// W waves share a row of up to 512 W C values; a block has four waves (W <= 4) or sixteen.
-template <int W, int C, bool GELU, bool GROUPED>
-__global__ __launch_bounds__(W <= 4 ? 256 : 64 * W)
+// GELU costs 20 vector instructions' time a value (75600 x 13824: 1026 us for what memory gives in 665), but it is a function of 65 536
+// values: one block per CU computes them all once, in 128 KB of LDS, and then looks its values up (BY_TABLE; the same function, the same bits).
+enum Activation { NO_GELU, GELU, GELU_BY_TABLE };
+
+// W waves share a row of up to 512 W C values; a block has four waves, or sixteen (W = 16, and with the table).
+template <int W, int C, int ACT, bool GROUPED>
+__global__ __launch_bounds__(W <= 4 && ACT != GELU_BY_TABLE ? 256 : 1024)
 void quantize_int8_kernel(const QuantInt8 q, const int run) {
-    constexpr int NW = W <= 4 ? 4 : W, TEAMS = NW / W;               // teams of W waves, each with rows of its own
+    constexpr int NW = W <= 4 && ACT != GELU_BY_TABLE ? 4 : 16, TEAMS = NW / W;          // teams of W waves, each with rows of its own
     __shared__ uint32_t part[2][NW];
+    __shared__ uint32_t table[ACT == GELU_BY_TABLE ? 32768 : 1];      // bf16(gelu(.)) of every bf16 value, two a word
+    static_assert(ACT != GELU_BY_TABLE || !GROUPED, "the table's blocks take longer runs than have a lane a row");
+    if constexpr (ACT == GELU_BY_TABLE) {
+        for (uint32_t i = threadIdx.x; i < 32768; i += 64 * NW) table[i] = gelu_tanh_bf16x2(2 * i | (2 * i + 1) << 16);
+        __syncthreads();
+    }
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int team = wave / W, tw = wave % W;
@@ -99,7 +109,11 @@ void quantize_int8_kernel(const QuantInt8 q, const int run) {
             uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if constexpr (GELU) w[j] = gelu_tanh_bf16x2(w[j]);
+                if constexpr (ACT == GELU) w[j] = gelu_tanh_bf16x2(w[j]);
+                if constexpr (ACT == GELU_BY_TABLE) {
+                    const uint16_t* const t = reinterpret_cast<const uint16_t*>(table);
+                    w[j] = t[w[j] & 0xffff] | (uint32_t)t[w[j] >> 16] << 16;
+                }
                 xs[c][2 * j] = bf16lo_f(w[j]);
                 xs[c][2 * j + 1] = bf16hi_f(w[j]);
             }
@@ -128,7 +142,7 @@ void quantize_int8_kernel(const QuantInt8 q, const int run) {
         }
         if (!owned) continue;
         const bool finite = top < 0x7f800000u;
-        const float rho = bits_f((uint32_t)__builtin_amdgcn_readlane((int)f_bits(ratios), i));
+        const float rho = q.row_rho ? bits_f((uint32_t)__builtin_amdgcn_readlane((int)f_bits(ratios), i)) : q.rho;
         float s = __fdiv_rn(__fmul_rn(rho, bits_f(top)), QMAX8);
         const bool fine = finite && s >= 1.17549435e-38f;
         const float inv = fine ? __fdiv_rn(1.0f, s) : 0.0f;
@@ -154,19 +168,19 @@ void quantize_int8_kernel(const QuantInt8 q, const int run) {
 template <int W, int C>
 hipError_t launch_row(const QuantInt8& q, const bool gelu, hipStream_t stream) {
     constexpr int TEAMS = W <= 4 ? 4 / W : 1, THREADS = W <= 4 ? 256 : 64 * W;
-    // eight blocks a CU, then longer runs of rows
+    auto go = [&](auto kernel, const int teams, const int threads, const int64_t run) {
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)((q.M + teams * run - 1) / (teams * run))), dim3(threads), 0, stream, q, (int)run);
+        return hipGetLastError();
+    };
+    // eight blocks a CU, then longer runs of rows (at most 64: a lane holds each row's token and ratio)
     int64_t run = q.M / (TEAMS * 2048);
     run = run < 1 ? 1 : run > 16 ? 16 : run;
-    const int64_t blocks = (q.M + TEAMS * run - 1) / (TEAMS * run);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(THREADS), 0, stream, q, (int)run); };
-    if (q.groups.offsets) {
-        if (gelu) go(quantize_int8_kernel<W, C, true, true>);
-        else go(quantize_int8_kernel<W, C, false, true>);
-    } else {
-        if (gelu) go(quantize_int8_kernel<W, C, true, false>);
-        else go(quantize_int8_kernel<W, C, false, false>);
-    }
-    return hipGetLastError();
+    if (q.groups.offsets) return gelu ? go(quantize_int8_kernel<W, C, GELU, true>, TEAMS, THREADS, run) : go(quantize_int8_kernel<W, C, NO_GELU, true>, TEAMS, THREADS, run);
+    if (!gelu) return go(quantize_int8_kernel<W, C, NO_GELU, false>, TEAMS, THREADS, run);
+    // the table takes a block 10 us
+    if (q.M * q.K < (int64_t)1 << 27) return go(quantize_int8_kernel<W, C, GELU, false>, TEAMS, THREADS, run);
+    constexpr int TABLE_TEAMS = 16 / W;
+    return go(quantize_int8_kernel<W, C, GELU_BY_TABLE, false>, TABLE_TEAMS, 1024, (q.M + TABLE_TEAMS * 256 - 1) / (TABLE_TEAMS * 256));
 }
 
 }  // namespace

@@ -129,8 +129,25 @@ def test_gelu_in_front():
     assert torch.equal(lin.forward(x, 0.9, gelu=True), svdq.linear_w8a8(qx, sx, lin.qw, lin.sw, lin.bias))
 
 
+@pytest.mark.parametrize("M,K", [(262200, 512), (140000, 1008), (70001, 2048), (33000, 4112), (20000, 8192), (9800, 13824), (5000, 32768)])
+def test_gelu_of_many_tokens(M, K):
+    """Where there are many the activation comes from a table: the same codes, and on every bf16 value, NaN rows and all."""
+    x = torch.randn((M, K), generator=torch.Generator("cuda").manual_seed(K), device="cuda", dtype=BF16) * 2
+    every = torch.arange(-32768, 32768, dtype=torch.int32).to(torch.int16).view(BF16).cuda()
+    every = every[every.isfinite()][:65024 // K * K if K < 65024 else K].view(-1, K)
+    x[-len(every):] = every
+    x[5, 3] = float("nan")
+    qx, sx = svdq.quantize_act_int8(x, None, 0.9, gelu=True)
+    for rows in (slice(0, 40), slice(M // 2, M // 2 + 40), slice(M - len(every) - 3, M)):
+        check_quantised(qx[rows], sx[rows], *quantise64(svdq.debug_gelu(x[rows]), None, 0.9))
+        few = svdq.quantize_act_int8(x[rows].contiguous(), None, 0.9, gelu=True)          # without the table
+        assert torch.equal(few[0], qx[rows]) and torch.equal(few[1].view(I32), sx[rows].view(I32))
+
+
 SHAPES = [(1, 1, 16), (1, 129, 128), (3, 5, 144), (2, 5120, 5120), (7, 1000, 13824), (16, 512, 4096), (17, 640, 1040), (33, 100, 16), (64, 64, 64), (65, 72, 80), (100, 4999, 272),
-          (128, 128, 128), (129, 257, 272), (200, 300, 4112), (300, 2048, 2048), (513, 771, 400), (1000, 1000, 1008), (2305, 515, 512), (4097, 2560, 640), (1, 30720, 160), (40, 8, 32768)]
+          (128, 128, 128), (129, 257, 272), (200, 300, 4112), (300, 2048, 2048), (513, 771, 400), (1000, 1000, 1008), (2305, 515, 512), (4097, 2560, 640), (1, 30720, 160), (40, 8, 32768),
+          # several rounds of the largest tiles, K of two stages and more, whole and not
+          (17000, 2048, 256), (20001, 2100, 272), (30000, 1290, 640), (9000, 5120, 384)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -190,7 +207,7 @@ def check_grouped(y, q, s, offsets, qw, sw, bias):
 
 
 @pytest.mark.parametrize("M,E,N,K", [(1, 1, 16, 16), (1, 64, 200, 256), (5, 3, 33, 48), (32, 128, 320, 512), (60, 7, 130, 272), (64, 1, 128, 128), (300, 2, 257, 400), (700, 65, 100, 144),
-                                     (1000, 9, 1030, 640), (2500, 3, 520, 1040), (4096, 1024, 24, 32), (9000, 5, 768, 512)])
+                                     (1000, 9, 1030, 640), (2500, 3, 520, 1040), (4096, 1024, 24, 32), (9000, 5, 768, 512), (20000, 3, 2100, 400), (18000, 64, 3000, 256), (18000, 65, 3000, 128)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_grouped_product(M, E, N, K, dtype):
     """Ragged and empty experts; rows in front of the first and behind the last expert stay as they were."""
