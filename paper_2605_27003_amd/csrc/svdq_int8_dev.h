@@ -12,10 +12,15 @@ constexpr float QMAX8 = 127.0f;  // codes are symmetric: -128 is not used
 // Number of the first offset past a row, E + 1 if there is none: the row is the expert's before it (the running maximum of the offsets passes
 // the row where the first offset does).  Wave-uniform; all lanes take part.
 __device__ __forceinline__ int first_offset_past(const Groups& g, const int64_t row, const int lane) {
-    for (int j0 = 0; j0 <= g.E; j0 += 64) {
-        const int j = j0 + lane;
-        const uint64_t past = __ballot(j <= g.E && g.offsets[j < g.E ? j : g.E] > row);
-        if (past) return j0 + __builtin_ctzll(past);
+    for (int j0 = 0; j0 <= g.E; j0 += 256) {                          // four loads under way at a time
+        int o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = g.offsets[j0 + 64 * k + lane < g.E ? j0 + 64 * k + lane : g.E];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint64_t past = __ballot(j0 + 64 * k + lane <= g.E && o[k] > row);
+            if (past) return j0 + 64 * k + __builtin_ctzll(past);
+        }
     }
     return g.E + 1;
 }

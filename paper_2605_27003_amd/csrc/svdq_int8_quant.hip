@@ -166,35 +166,60 @@ void quantize_int8_kernel(const QuantInt8 q, const int run) {
 }
 
 template <int W, int C>
-hipError_t launch_row(const QuantInt8& q, const bool gelu, hipStream_t stream) {
+hipError_t launch_rows(const QuantInt8& q, const bool gelu, hipStream_t stream) {
     constexpr int TEAMS = W <= 4 ? 4 / W : 1, THREADS = W <= 4 ? 256 : 64 * W;
-    auto go = [&](auto kernel, const int teams, const int threads, const int64_t run) {
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)((q.M + teams * run - 1) / (teams * run))), dim3(threads), 0, stream, q, (int)run);
+    // eight blocks a CU, then longer runs of rows (at most 64: a lane holds each row's token and ratio); grouped, where a block begins with its
+    // expert, token and smoothing vector one after the other, four
+    int64_t run = q.M / (TEAMS * (q.groups.offsets ? 1024 : 2048));
+    run = run < 1 ? 1 : run > 16 ? 16 : run;
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)((q.M + TEAMS * run - 1) / (TEAMS * run))), dim3(THREADS), 0, stream, q, (int)run);
         return hipGetLastError();
     };
-    // eight blocks a CU, then longer runs of rows (at most 64: a lane holds each row's token and ratio)
-    int64_t run = q.M / (TEAMS * 2048);
-    run = run < 1 ? 1 : run > 16 ? 16 : run;
-    if (q.groups.offsets) return gelu ? go(quantize_int8_kernel<W, C, GELU, true>, TEAMS, THREADS, run) : go(quantize_int8_kernel<W, C, NO_GELU, true>, TEAMS, THREADS, run);
-    if (!gelu) return go(quantize_int8_kernel<W, C, NO_GELU, false>, TEAMS, THREADS, run);
-    // the table takes a block 10 us
-    if (q.M * q.K < (int64_t)1 << 27) return go(quantize_int8_kernel<W, C, GELU, false>, TEAMS, THREADS, run);
-    constexpr int TABLE_TEAMS = 16 / W;
-    return go(quantize_int8_kernel<W, C, GELU_BY_TABLE, false>, TABLE_TEAMS, 1024, (q.M + TABLE_TEAMS * 256 - 1) / (TABLE_TEAMS * 256));
+    if (q.groups.offsets) return gelu ? go(quantize_int8_kernel<W, C, GELU, true>) : go(quantize_int8_kernel<W, C, NO_GELU, true>);
+    return gelu ? go(quantize_int8_kernel<W, C, GELU, false>) : go(quantize_int8_kernel<W, C, NO_GELU, false>);
+}
+
+template <int W, int C>
+hipError_t launch_by_table(const QuantInt8& q, hipStream_t stream) {
+    constexpr int TEAMS = 16 / W;
+    const int64_t run = (q.M + TEAMS * 256 - 1) / (TEAMS * 256);
+    hipLaunchKernelGGL((quantize_int8_kernel<W, C, GELU_BY_TABLE, false>), dim3((uint32_t)((q.M + TEAMS * run - 1) / (TEAMS * run))), dim3(1024), 0, stream, q, (int)run);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_quantize_int8(const QuantInt8& q, bool gelu, hipStream_t stream) {
     const int chunks = q.K >> 3;
-    if (chunks <= 64) return launch_row<1, 1>(q, gelu, stream);
-    if (chunks <= 128) return launch_row<1, 2>(q, gelu, stream);
-    if (chunks <= 256) return launch_row<4, 1>(q, gelu, stream);
-    if (chunks <= 512) return launch_row<4, 2>(q, gelu, stream);
-    if (chunks <= 768) return launch_row<4, 3>(q, gelu, stream);
-    if (chunks <= 1024) return launch_row<4, 4>(q, gelu, stream);
-    if (chunks <= 2048) return launch_row<16, 2>(q, gelu, stream);
-    return launch_row<16, 4>(q, gelu, stream);
+    if (gelu && !q.groups.offsets && q.M * q.K >= (int64_t)1 << 27) {        // the table takes a block 10 us
+        if (chunks <= 64) return launch_by_table<1, 1>(q, stream);
+        if (chunks <= 128) return launch_by_table<1, 2>(q, stream);
+        if (chunks <= 256) return launch_by_table<1, 4>(q, stream);
+        if (chunks <= 512) return launch_by_table<4, 2>(q, stream);
+        if (chunks <= 768) return launch_by_table<4, 3>(q, stream);
+        if (chunks <= 1024) return launch_by_table<4, 4>(q, stream);
+        if (chunks <= 2048) return launch_by_table<16, 2>(q, stream);
+        return launch_by_table<16, 4>(q, stream);
+    }
+    if (chunks <= 64) return launch_rows<1, 1>(q, gelu, stream);
+    if (chunks <= 128) return launch_rows<1, 2>(q, gelu, stream);
+    if (q.M >= 2048) {
+        // A row costs each of its waves the maximum's exchange and two divisions, as much as sixteen values a lane: few waves, many values.
+        if (chunks <= 192) return launch_rows<1, 3>(q, gelu, stream);
+        if (chunks <= 256) return launch_rows<1, 4>(q, gelu, stream);
+        if (chunks <= 512) return launch_rows<2, 4>(q, gelu, stream);
+        if (chunks <= 640) return launch_rows<2, 5>(q, gelu, stream);
+        if (chunks <= 1024) return launch_rows<4, 4>(q, gelu, stream);
+        if (chunks <= 1280) return launch_rows<4, 5>(q, gelu, stream);
+        if (chunks <= 1792) return launch_rows<4, 7>(q, gelu, stream);
+    }
+    // few rows: what counts is one row's time
+    if (chunks <= 256) return launch_rows<4, 1>(q, gelu, stream);
+    if (chunks <= 512) return launch_rows<4, 2>(q, gelu, stream);
+    if (chunks <= 768) return launch_rows<4, 3>(q, gelu, stream);
+    if (chunks <= 2048) return launch_rows<16, 2>(q, gelu, stream);
+    return launch_rows<16, 4>(q, gelu, stream);
 }
 
 }  // namespace svdq
