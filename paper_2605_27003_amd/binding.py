@@ -697,47 +697,47 @@ def _gpu(t):
     raise ValueError(f"tensors on the current GPU are needed, not on {t.device}")
 
 
+_BF16, _F32, _I8, _I32 = torch.bfloat16, torch.float32, torch.int8, torch.int32
+
+
 def _refuse(name, t, dtype, shape, gpu):
     wanted = " or ".join(map(str, dtype)) if isinstance(dtype, tuple) else dtype
     raise ValueError(f"{name}: {wanted} of shape {shape} is needed, rows of consecutive values, on GPU {gpu} (the current one); "
                      f"got {t.dtype} of shape {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
 
 
-def _vector(name, t, dtype, shape, gpu):
-    """A contiguous tensor of this type and shape on GPU `gpu` -> its address."""
+def _vector(name, t, dtype, n, gpu):
+    """A contiguous tensor of this type and n elements on GPU `gpu` -> its address."""
+    if t.dtype is not dtype or t.numel() != n or t.get_device() != gpu or not t.is_contiguous():
+        _refuse(name, t, dtype, f"[{n}]", gpu)
+    return t.data_ptr()
+
+
+def _tensor(name, t, dtype, shape, gpu):
+    """The same with its shape."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != gpu or not t.is_contiguous():
         _refuse(name, t, dtype, shape, gpu)
     return t.data_ptr()
 
 
-def _optional(name, t, dtype, shape, gpu):
-    return None if t is None else _vector(name, t, dtype, shape, gpu)
-
-
 def _matrix(name, t, dtypes, gpu, cols=None):
     """A matrix on GPU `gpu` whose rows of consecutive values may be further apart than they are long -> (rows, columns, row stride)."""
-    if t.dim() != 2 or t.dtype not in dtypes or t.get_device() != gpu or (cols is not None and t.shape[1] != cols):
+    if t.dim() != 2 or t.dtype not in dtypes or t.get_device() != gpu:
         _refuse(name, t, dtypes, ("any", "any" if cols is None else cols), gpu)
-    rows, cols = t.shape
+    rows, n = t.shape
+    ld, one = t.stride()
     if rows <= 1:
-        ld = (cols + 7) & ~7
-    else:
-        ld = t.stride(0)
-        if ld < cols:
-            _refuse(name, t, dtypes, (rows, cols), gpu)
-    if cols > 1 and t.stride(1) != 1:
-        _refuse(name, t, dtypes, (rows, cols), gpu)
-    return rows, cols, ld
-
-
-_BF16, _F32, _I8, _I32 = torch.bfloat16, torch.float32, torch.int8, torch.int32
+        ld = (n + 7) & ~7
+    if (cols is not None and n != cols) or ld < n or (one != 1 and n > 1):
+        _refuse(name, t, dtypes, (rows, n if cols is None else cols), gpu)
+    return rows, n, ld
 
 
 def _quantize_int8_out(out, M, K, x, gpu):
     if out is None:
         return torch.empty((M, K), dtype=_I8, device=x.device), torch.empty(M, dtype=_F32, device=x.device)
-    _vector("out[0]", out[0], _I8, (M, K), gpu)
-    _vector("out[1]", out[1], _F32, (M,), gpu)
+    _tensor("out[0]", out[0], _I8, (M, K), gpu)
+    _vector("out[1]", out[1], _F32, M, gpu)
     return out
 
 
@@ -746,7 +746,7 @@ def quantize_act_int8(x_bf16, inv_lambda=None, rho=1.0, gelu=False, out=None):
     (rho max|.|) / 127 a token; gelu=True: of gelu(x)."""
     gpu = _gpu(x_bf16)
     M, K, ldx = _matrix("x", x_bf16, (_BF16,), gpu)
-    il = _optional("inv_lambda", inv_lambda, _F32, (K,), gpu)
+    il = None if inv_lambda is None else _vector("inv_lambda", inv_lambda, _F32, K, gpu)
     qx, sx = _quantize_int8_out(out, M, K, x_bf16, gpu)
     if M:                            # an empty tensor has no address
         _check((_lib or load_library()).svdq_quantize_act_int8(x_bf16.data_ptr(), ldx, il, float(rho), 1 if gelu else 0, M, K, qx.data_ptr(), sx.data_ptr(),
@@ -772,11 +772,11 @@ def linear_w8a8(qx, sx, qw, sw, bias=None, out=None, out_dtype=torch.bfloat16):
     if qx.dim() != 2 or qw.dim() != 2:
         _refuse("qx, qw", qx if qx.dim() != 2 else qw, _I8, ("any", "any"), gpu)
     (M, K), N = qx.shape, qw.shape[0]
-    args = (_vector("qx", qx, _I8, (M, K), gpu), _vector("sx", sx, _F32, (M,), gpu), _vector("qw", qw, _I8, (N, K), gpu),
-            _vector("sw", sw, _F32, (N,), gpu), _optional("bias", bias, _F32, (N,), gpu))
+    pq, ps, pw, pc = _vector("qx", qx, _I8, M * K, gpu), _vector("sx", sx, _F32, M, gpu), _tensor("qw", qw, _I8, (N, K), gpu), _vector("sw", sw, _F32, N, gpu)
+    pb = None if bias is None else _vector("bias", bias, _F32, N, gpu)
     y, ldy, code = _linear_out(out, M, N, out_dtype, qx, gpu)
     if M:
-        _check((_lib or load_library()).svdq_linear_w8a8(*args, M, N, K, y.data_ptr(), ldy, code, _raw_stream()), "svdq_linear_w8a8")
+        _check((_lib or load_library()).svdq_linear_w8a8(pq, ps, pw, pc, pb, M, N, K, y.data_ptr(), ldy, code, _raw_stream()), "svdq_linear_w8a8")
     return y
 
 
@@ -784,7 +784,7 @@ def _row_rho(rho, M, gpu):
     """(the ratio of all rows, or the address of every row's)"""
     if not torch.is_tensor(rho):
         return float(rho), None
-    return 1.0, _vector("rho", rho, _F32, (M,), gpu)
+    return 1.0, _vector("rho", rho, _F32, M, gpu)
 
 
 def quantize_act_int8_grouped(x_bf16, offsets, inv_lambda=None, rho=1.0, rows=None, gelu=False, out=None):
@@ -794,8 +794,8 @@ def quantize_act_int8_grouped(x_bf16, offsets, inv_lambda=None, rho=1.0, rows=No
     gpu = _gpu(x_bf16)
     x_rows, K, ldx = _matrix("x", x_bf16, (_BF16,), gpu)
     M, E = (x_rows if rows is None else rows.numel()), offsets.numel() - 1
-    o, r = _vector("offsets", offsets, _I32, (E + 1,), gpu), _optional("rows", rows, _I32, (M,), gpu)
-    il = _optional("inv_lambda", inv_lambda, _F32, (E, K), gpu)
+    o, r = _vector("offsets", offsets, _I32, E + 1, gpu), None if rows is None else _vector("rows", rows, _I32, M, gpu)
+    il = None if inv_lambda is None else _tensor("inv_lambda", inv_lambda, _F32, (E, K), gpu)
     ratio, row_rho = _row_rho(rho, M, gpu)
     qx, sx = _quantize_int8_out(out, M, K, x_bf16, gpu)
     if M:
@@ -812,11 +812,12 @@ def linear_w8a8_grouped(qx, sx, offsets, qw, sw, bias=None, out=None, out_dtype=
     if qx.dim() != 2 or qw.dim() != 3:
         _refuse("qx, qw", qx if qx.dim() != 2 else qw, _I8, "[M, K], [E, N, K]", gpu)
     (M, K), (E, N, _) = qx.shape, qw.shape
-    args = (_vector("qx", qx, _I8, (M, K), gpu), _vector("sx", sx, _F32, (M,), gpu), _vector("qw", qw, _I8, (E, N, K), gpu),
-            _vector("sw", sw, _F32, (E, N), gpu), _optional("bias", bias, _F32, (E, N), gpu), _vector("offsets", offsets, _I32, (E + 1,), gpu))
+    pq, ps, pw = _vector("qx", qx, _I8, M * K, gpu), _vector("sx", sx, _F32, M, gpu), _tensor("qw", qw, _I8, (E, N, K), gpu)
+    pc, pb = _tensor("sw", sw, _F32, (E, N), gpu), None if bias is None else _tensor("bias", bias, _F32, (E, N), gpu)
+    o = _vector("offsets", offsets, _I32, E + 1, gpu)
     y, ldy, code = _linear_out(out, M, N, out_dtype, qx, gpu)
     if M:
-        _check((_lib or load_library()).svdq_linear_w8a8_grouped(*args, E, M, N, K, y.data_ptr(), ldy, code, _raw_stream()), "svdq_linear_w8a8_grouped")
+        _check((_lib or load_library()).svdq_linear_w8a8_grouped(pq, ps, pw, pc, pb, o, E, M, N, K, y.data_ptr(), ldy, code, _raw_stream()), "svdq_linear_w8a8_grouped")
     return y
 
 
@@ -845,8 +846,9 @@ class _W8A8:
         if qw.dim() != 2 + self.GROUPED:
             raise ValueError(f"qw: {'[E, N, K]' if self.GROUPED else '[N, K]'} is needed, not {tuple(qw.shape)}")
         lead, (N, K), gpu = tuple(qw.shape[:-2]), qw.shape[-2:], qw.get_device()
-        layer = _LayerInt8(lead[0] if lead else 0, N, K, _optional("inv_lambda", inv_lambda, _F32, lead + (K,), gpu), _vector("qw", qw, _I8, lead + (N, K), gpu),
-                           _vector("sw", sw, _F32, lead + (N,), gpu), _optional("bias", bias, _F32, lead + (N,), gpu))
+        layer = _LayerInt8(lead[0] if lead else 0, N, K, None if inv_lambda is None else _tensor("inv_lambda", inv_lambda, _F32, lead + (K,), gpu),
+                           _tensor("qw", qw, _I8, lead + (N, K), gpu), _tensor("sw", sw, _F32, lead + (N,), gpu),
+                           None if bias is None else _tensor("bias", bias, _F32, lead + (N,), gpu))
         layer.address, layer.shape = ctypes.addressof(layer), (layer.E, N, K, gpu)
         self._held = (tensors, layer)
         return layer
@@ -893,6 +895,6 @@ class W8A8Experts(_W8A8):
         expert owns are not written (without `out`: hold anything)."""
         layer, gpu = self._descriptor(), _gpu(x_bf16)
         M = x_bf16.shape[0] if rows is None else rows.numel()
-        o, r = _vector("offsets", offsets, _I32, (layer.shape[0] + 1,), gpu), _optional("rows", rows, _I32, (M,), gpu)
+        o, r = _vector("offsets", offsets, _I32, layer.shape[0] + 1, gpu), None if rows is None else _vector("rows", rows, _I32, M, gpu)
         ratio, row_rho = _row_rho(rho, M, gpu)
         return self._forward(x_bf16, layer, gpu, r, o, ratio, row_rho, gelu, M, out)

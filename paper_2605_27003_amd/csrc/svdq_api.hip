@@ -8,6 +8,7 @@
 #include <cstring>
 
 #include "svdq_int8.h"
+#include "svdq_int8_plan.h"
 #include "svdq_kernels.h"
 #include "svdq_mx_plan.h"
 
@@ -578,14 +579,17 @@ static int quantize_int8_check(const svdq::QuantInt8& q) {
     return q.M > SVDQ_MAX_M ? SVDQ_ERR_UNSUPPORTED_SHAPE : SVDQ_OK;
 }
 
-static int gemm_int8_check(const svdq::GemmInt8& g, int out_dtype) {
+// plan: the tiles that the product takes
+static int gemm_int8_check(const svdq::GemmInt8& g, int out_dtype, svdq::Int8Plan& plan) {
     if (!g.qx || !g.sx || !g.qw || !g.sw || !g.y || g.M < 0) return SVDQ_ERR_INVALID_ARG;
     if (out_dtype != SVDQ_OUT_BF16 && out_dtype != SVDQ_OUT_F32) return SVDQ_ERR_INVALID_ARG;
     if (g.N <= 0 || g.K <= 0 || g.K % 16 || g.K > SVDQ_MAX_K_INT8 || g.ldy < g.N) return SVDQ_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(g.qx) || !aligned16(g.qw) || !aligned4(g.sx) || !aligned4(g.sw) || !aligned4(g.bias)) return SVDQ_ERR_UNSUPPORTED_SHAPE;
     if ((uintptr_t)g.y & (out_dtype == SVDQ_OUT_F32 ? 3u : 1u)) return SVDQ_ERR_UNSUPPORTED_SHAPE;
-    if (g.M > SVDQ_MAX_M || !svdq::gemm_int8_fits(g)) return SVDQ_ERR_UNSUPPORTED_SHAPE;
-    return SVDQ_OK;
+    if (g.M > SVDQ_MAX_M) return SVDQ_ERR_UNSUPPORTED_SHAPE;
+    if (g.M == 0) return SVDQ_OK;
+    plan = svdq::int8_plan(g.M, g.N, g.K, g.groups.offsets ? g.groups.E : 0, out_dtype == SVDQ_OUT_F32);
+    return plan.cost < 0.0 ? SVDQ_ERR_UNSUPPORTED_SHAPE : SVDQ_OK;
 }
 
 static int groups_check(const int32_t* offsets, int E) {
@@ -601,10 +605,11 @@ static int quantize_int8(const svdq::QuantInt8& q, int gelu, void* stream) {
 }
 
 static int linear_int8(const svdq::GemmInt8& g, int out_dtype, void* stream) {
-    if (int e = gemm_int8_check(g, out_dtype)) return e;
+    svdq::Int8Plan plan{};
+    if (int e = gemm_int8_check(g, out_dtype, plan)) return e;
     if (g.M == 0) return SVDQ_OK;
     if (int a = check_arch()) return a;
-    return hip_status(svdq::launch_gemm_int8(g, out_dtype == SVDQ_OUT_F32, (hipStream_t)stream));
+    return hip_status(svdq::launch_gemm_int8(g, plan, out_dtype == SVDQ_OUT_F32, (hipStream_t)stream));
 }
 
 int svdq_quantize_act_int8(const void* x_bf16, int64_t ldx, const float* inv_lambda, float rho, int gelu,
@@ -641,11 +646,12 @@ int svdq_layer_int8_forward(const svdq_layer_int8* L, const void* x_bf16, int64_
     const svdq::QuantInt8 q{x_bf16, ldx, rows, x_rows, L->inv_lambda, row_rho, rho, L->K, M, qx, sx, groups};
     const svdq::GemmInt8 g{qx, sx, L->qw, L->sw, L->bias, y, ldy, M, L->N, L->K, groups};
     if (int e = quantize_int8_check(q)) return e;
-    if (int e = gemm_int8_check(g, SVDQ_OUT_BF16)) return e;
+    svdq::Int8Plan plan{};
+    if (int e = gemm_int8_check(g, SVDQ_OUT_BF16, plan)) return e;
     if (M == 0) return SVDQ_OK;
     if (int a = check_arch()) return a;
     const hipError_t e = svdq::launch_quantize_int8(q, gelu != 0, (hipStream_t)stream);
-    return hip_status(e != hipSuccess ? e : svdq::launch_gemm_int8(g, false, (hipStream_t)stream));
+    return hip_status(e != hipSuccess ? e : svdq::launch_gemm_int8(g, plan, false, (hipStream_t)stream));
 }
 
 size_t svdq_gptq_workspace_bytes(int N, int K) {

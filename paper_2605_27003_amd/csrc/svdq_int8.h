@@ -39,9 +39,8 @@ struct GemmInt8 {
     int N, K;
     Groups groups;
 };
-bool gemm_int8_fits(const GemmInt8& g);                 // whether the grid can be numbered
-hipError_t launch_gemm_int8(const GemmInt8& g, bool out_f32, hipStream_t stream);
 struct Int8Plan;
+hipError_t launch_gemm_int8(const GemmInt8& g, const Int8Plan& p, bool out_f32, hipStream_t stream);
 hipError_t launch_gemm_int8_few(const GemmInt8& g, const Int8Plan& p, bool out_f32, hipStream_t stream);     // the few-token kernel's tiles
 
 }  // namespace svdq

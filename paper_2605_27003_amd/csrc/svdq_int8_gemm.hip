@@ -102,23 +102,26 @@ struct TileStore {
                     }
                 } else {
                     // four bytes a lane, or two: consecutive lanes store consecutive elements
-                    constexpr int WORDS = COLS * (int)sizeof(T) / 4;
-                    const int n = ROWS * WORDS * (unit == 4 ? 1 : 2), per = WORDS * (unit == 4 ? 1 : 2);
-                    for (int i = lane; i < n; i += 64) {
-                        const int row = i / per, c = i - row * per;
-                        if (m0 * I + row >= rows) break;
-                        T* const p = y0 + (int64_t)(m0 * I + row) * ldy;
-                        const uint32_t v = lds_read4(region + row * PITCH + (unit == 4 ? c : c >> 1) * 4);
-                        if constexpr (sizeof(T) == 4) {
-                            if (c < left) p[c] = v;
-                        } else if (unit == 4 && 2 * c + 1 < left) {
-                            *reinterpret_cast<uint32_t*>(p + 2 * c) = v;
-                        } else if (unit == 4) {
-                            if (2 * c < left) p[2 * c] = (T)v;
-                        } else if (c < left) {
-                            p[c] = (T)(v >> (16 * (c & 1)));
+                    auto by = [&](auto PERC) {
+                        constexpr int PER = decltype(PERC)::value, E = COLS / PER;       // stores a row, elements each
+#pragma unroll 4
+                        for (int i = lane; i < ROWS * PER; i += 64) {
+                            const int row = i / PER, c = i % PER;
+                            if (m0 * I + row >= rows) break;
+                            T* const p = y0 + (int64_t)(m0 * I + row) * ldy + c * E;
+                            const uint32_t v = lds_read4(region + row * PITCH + (c * E * (int)sizeof(T) & ~3));
+                            if constexpr (E * sizeof(T) == 2) {
+                                if (c < left) *p = (T)(v >> (16 * (c & 1)));
+                            } else if constexpr (E == 2) {
+                                if (2 * c + 1 < left) *reinterpret_cast<uint32_t*>(p) = v;
+                                else if (2 * c < left) *p = (T)v;
+                            } else {
+                                if (c < left) *p = (T)v;
+                            }
                         }
-                    }
+                    };
+                    if (sizeof(T) == 4 || unit == 2) by(IC<COLS>{});
+                    else by(IC<COLS / 2>{});
                 }
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
                 __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -142,6 +145,7 @@ struct Int8Tile {
 // A(s + DEPTH) during its first three quarters (its place has been free since the barrier of stage s - 1) and W(s + DEPTH) during its
 // last, where W(s) stood: requests that come all at once behind the barrier take longer than the instructions that they stand between
 // (with a place less and all of them there, 256 x 256 tiles took 6 % longer at K = 13824).
+// TAIL: K is no multiple of a stage.  The last stage's pieces beyond K repeat the row's last piece, and count as zeros in the weights' operand.
 template <class G, bool TAIL, bool GROUPED, class T>
 __global__ __launch_bounds__(G::THREADS, 1)
 void gemm_int8_kernel(const GemmInt8 g) {
@@ -179,15 +183,16 @@ void gemm_int8_kernel(const GemmInt8 g) {
     for (int j = 0; j < NA; ++j) rows_of(va[j], pa[j], block_a(j), m_end - 1 - m0);
 #pragma unroll
     for (int j = 0; j < NB; ++j) rows_of(vw[j], pw[j], block_w(j), N - 1 - n0);
-    auto request = [&](const int8_t* base, uint32_t v, const uint32_t piece, const int s, const uint32_t to) {
-        if constexpr (TAIL) {
+    // EDGE: of what may be the last stage, whose pieces can lie beyond K
+    auto request = [&](auto EDGEC, const int8_t* base, uint32_t v, const uint32_t piece, const int s, const uint32_t to) {
+        if constexpr (TAIL && decltype(EDGEC)::value) {
             const int left = (K >> 4) - 8 * s - 1, over = (int)piece - left;
             if (over > 0) v -= over * 16;
         }
         dma16(base + (int64_t)s * BK, v, to);
     };
-    auto request_a = [&](const int s, const uint32_t to, const int j) { request(abase, va[j], pa[j], s, to + block_a(j) * 1024); };
-    auto request_w = [&](const int s, const uint32_t to, const int j) { request(wbase, vw[j], pw[j], s, to + block_w(j) * 1024); };
+    auto request_a = [&](auto EDGEC, const int s, const uint32_t to, const int j) { request(EDGEC, abase, va[j], pa[j], s, to + block_a(j) * 1024); };
+    auto request_w = [&](auto EDGEC, const int s, const uint32_t to, const int j) { request(EDGEC, wbase, vw[j], pw[j], s, to + block_w(j) * 1024); };
     auto next_a = [&](const uint32_t c) { return c == ring_a + DEPTH * G::A ? ring_a : c + G::A; };
     auto next_w = [&](const uint32_t c) { return c == ring_w + (DEPTH - 1) * G::W ? ring_w : c + G::W; };
 
@@ -205,14 +210,14 @@ void gemm_int8_kernel(const GemmInt8 g) {
     };
     typedef const volatile __attribute__((address_space(3))) int4v lds_i4;
     auto fetch = [&](const uint32_t from, const int block) { return *reinterpret_cast<lds_i4*>((lds_byte*)(uintptr_t)from + block * I * BK); };
-    auto read = [&](Operands& o, const uint32_t fa, const uint32_t fw, const int s, const int kk, const int r) {
+    auto read = [&](auto EDGEC, Operands& o, const uint32_t fa, const uint32_t fw, const int s, const int kk, const int r) {
         if (r >= 1 && r <= MT) {                                      // in the order of their use
             o.x[r - 1] = fetch(fa, r - 1);
             return;
         }
         const int ni = r == 0 ? 0 : r - MT;
         o.w[ni] = fetch(fw, ni);
-        if constexpr (TAIL) {
+        if constexpr (TAIL && decltype(EDGEC)::value) {
             if (8 * s + PS * kk + lk >= (K >> 4)) o.w[ni] = int4v{0, 0, 0, 0};
         }
     };
@@ -228,9 +233,9 @@ void gemm_int8_kernel(const GemmInt8 g) {
     for (int s = 0; s < DEPTH; ++s)
         if (s < nstages) {
 #pragma unroll
-            for (int j = 0; j < NA; ++j) request_a(s, ring_a + s * G::A, j);
+            for (int j = 0; j < NA; ++j) request_a(IC<1>{}, s, ring_a + s * G::A, j);
 #pragma unroll
-            for (int j = 0; j < NB; ++j) request_w(s, ring_w + s * G::W, j);
+            for (int j = 0; j < NB; ++j) request_w(IC<1>{}, s, ring_w + s * G::W, j);
         }
     // wait for a stage with `behind` whole ones, at most DEPTH - 1, requested after it
     auto wait_for = [&](const int behind) {
@@ -245,11 +250,12 @@ void gemm_int8_kernel(const GemmInt8 g) {
     constexpr int T_ = MT * NT, READS = MT + NT, QUARTER = STEPS * T_ / 4;
     Operands op[2];
 #pragma unroll
-    for (int r = 0; r < READS; ++r) read(op[0], ring_a + rd_a[0], ring_w + rd_w[0], 0, 0, r);
+    for (int r = 0; r < READS; ++r) read(IC<1>{}, op[0], ring_a + rd_a[0], ring_w + rd_w[0], 0, 0, r);
 
     // A stage is STEPS k steps, of T_ instructions each; between those the reads of the next step's operands and the stage's requests.
     // Before its last quarter (when every wave has all of its operands) stand the wait for the next stage's rows and the barrier.
-    auto stage = [&](const int s, auto FILLC, auto LASTC) {
+    // EDGE: its requests may be the last stage's, or its reads.
+    auto stage = [&](const int s, auto FILLC, auto EDGEC, auto LASTC) {
         constexpr bool fill = decltype(FILLC)::value, last = decltype(LASTC)::value;
         const uint32_t na = next_a(cur_a), nw = next_w(cur_w), free_a = cur_a == ring_a ? ring_a + DEPTH * G::A : cur_a - G::A;
         auto instructions = [&](auto FROM, auto TO) {
@@ -266,14 +272,14 @@ void gemm_int8_kernel(const GemmInt8 g) {
                 if (!(next && last) && n >= r0)
 #pragma unroll
                     for (int r = (n - r0) * RP; r < (n - r0 + 1) * RP && r < READS; ++r)
-                        read(op[rk & 1], fa, fw, next ? s + 1 : s, rk, r);
+                        read(EDGEC, op[rk & 1], fa, fw, next ? s + 1 : s, rk, r);
                 if constexpr (fill) {                                 // request i of n stands behind instruction (i + 1/2) / n of its part
 #pragma unroll
                     for (int j = 0; j < NA; ++j)
-                        if (n == (2 * j + 1) * 3 * QUARTER / (2 * NA)) request_a(s + DEPTH, free_a, j);
+                        if (n == (2 * j + 1) * 3 * QUARTER / (2 * NA)) request_a(EDGEC, s + DEPTH, free_a, j);
 #pragma unroll
                     for (int j = 0; j < NB; ++j)
-                        if (n == 3 * QUARTER + j * QUARTER / NB) request_w(s + DEPTH, cur_w, j);
+                        if (n == 3 * QUARTER + j * QUARTER / NB) request_w(EDGEC, s + DEPTH, cur_w, j);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -288,8 +294,9 @@ void gemm_int8_kernel(const GemmInt8 g) {
         cur_w = nw;
     };
     int s = 0;
-    for (; s + DEPTH < nstages; ++s) stage(s, IC<1>{}, IC<0>{});
-    for (; s + 1 < nstages; ++s) stage(s, IC<0>{}, IC<0>{});
+    for (; s + DEPTH + (TAIL ? 1 : 0) < nstages; ++s) stage(s, IC<1>{}, IC<0>{}, IC<0>{});
+    if (TAIL && s + DEPTH < nstages) stage(s++, IC<1>{}, IC<1>{}, IC<0>{});
+    for (; s + 1 < nstages; ++s) stage(s, IC<0>{}, IC<1>{}, IC<0>{});
     // the last stage's requests are the tile's scales and biases, 64 values each, into the place behind its tokens'
     const uint32_t scales = next_a(cur_a);
     for (int j = wave; j < (int)G::SCALES / 256; j += G::NW) {
@@ -298,7 +305,7 @@ void gemm_int8_kernel(const GemmInt8 g) {
         const int i = (j - (tok ? 0 : bia ? BIAS0 : CHANNEL0)) * 64 + lane, end = tok ? m_end - 1 - m0 : N - 1 - n0;
         if (!bia || at.bias) dma4(tok ? g.sx + m0 : bia ? at.bias + n0 : at.sw + n0, (uint32_t)(i < end ? i : end) * 4, scales + j * 256);
     }
-    stage(s, IC<0>{}, IC<1>{});
+    stage(s, IC<0>{}, IC<1>{}, IC<1>{});
 
     const uintptr_t ends = reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)(g.ldy * (int64_t)sizeof(T));
     const int unit = (ends & 15) == 0 ? 16 : (ends & 3) == 0 ? 4 : 2;
@@ -326,10 +333,7 @@ hipError_t launch_tiles(const GemmInt8& g, const bool out_f32, hipStream_t strea
 
 }  // namespace
 
-bool gemm_int8_fits(const GemmInt8& g) { return g.M == 0 || int8_plan(g.M, g.N, g.K, g.groups.offsets ? g.groups.E : 0, false).cost >= 0.0; }
-
-hipError_t launch_gemm_int8(const GemmInt8& g, bool out_f32, hipStream_t stream) {
-    const Int8Plan p = int8_plan(g.M, g.N, g.K, g.groups.offsets ? g.groups.E : 0, out_f32);
+hipError_t launch_gemm_int8(const GemmInt8& g, const Int8Plan& p, bool out_f32, hipStream_t stream) {
     switch (p.tiles) {
         case Int8Tiles::T64x32: return launch_tiles<Int8Tile<64, 32, 2, 2, 4>>(g, out_f32, stream);
         case Int8Tiles::T64x64: return launch_tiles<Int8Tile<64, 64, 2, 2, 4>>(g, out_f32, stream);
