@@ -759,7 +759,7 @@ def _linear_out(out, M, N, out_dtype, like, gpu):
     if out is None:
         if out_dtype is not _BF16 and out_dtype is not _F32:
             raise ValueError(f"out_dtype: bfloat16 or float32, not {out_dtype}")
-        return torch.empty((M, N), dtype=out_dtype, device=like.device), N, OUT_F32 if out_dtype is _F32 else OUT_BF16
+        return torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=like.device), N, OUT_F32 if out_dtype is _F32 else OUT_BF16
     rows, _, ldy = _matrix("out", out, (_BF16, _F32), gpu, N)
     if rows != M:
         _refuse("out", out, (_BF16, _F32), (M, N), gpu)

@@ -650,6 +650,11 @@ int svdq_layer_int8_forward(const svdq_layer_int8* L, const void* x_bf16, int64_
     if (int e = gemm_int8_check(g, SVDQ_OUT_BF16, plan)) return e;
     if (M == 0) return SVDQ_OK;
     if (int a = check_arch()) return a;
+    // on its own input the output is written behind the quantise launch: in one launch, blocks of other channel tiles still read x
+    const int64_t read = rows ? x_rows : M;
+    const uintptr_t x0 = (uintptr_t)x_bf16, y0 = (uintptr_t)y;
+    const bool meet = read > 0 && x0 < y0 + 2 * ((uintptr_t)(M - 1) * ldy + L->N) && y0 < x0 + 2 * ((uintptr_t)(read - 1) * ldx + L->K);
+    if (!meet && svdq::layer_int8_fits(g)) return hip_status(svdq::launch_layer_int8(q, g, gelu != 0, (hipStream_t)stream));
     const hipError_t e = svdq::launch_quantize_int8(q, gelu != 0, (hipStream_t)stream);
     return hip_status(e != hipSuccess ? e : svdq::launch_gemm_int8(g, plan, false, (hipStream_t)stream));
 }

@@ -9,6 +9,35 @@ namespace svdq {
 constexpr int BK = 128;          // k (and bytes) of a row per stage of a product: one memory line
 constexpr float QMAX8 = 127.0f;  // codes are symmetric: -128 is not used
 
+// A row's scale from the bit pattern of its largest magnitude (a NaN's or an infinity's is past every finite one's), and what its values are
+// multiplied with; false: codes 0, the scale NaN where the row or its ratio is none, 0 where it would not be a normal number.
+__device__ __forceinline__ bool row_scale(const uint32_t top, const float rho, float& s, float& inv) {
+    const bool finite = top < 0x7f800000u;
+    s = __fdiv_rn(__fmul_rn(rho, bits_f(top)), QMAX8);
+    const bool fine = finite && s >= 1.17549435e-38f;
+    inv = fine ? __fdiv_rn(1.0f, s) : 0.0f;
+    if (!fine) s = finite && s == s ? 0.0f : bits_f(0x7fc00000u);
+    return fine;
+}
+// eight codes: clamped first, so that adding 1.5 2^23 rounds to the nearest whole number (ties to even) in the low bits
+__device__ __forceinline__ uint2 codes8(const float (&x)[8], const float inv, const bool fine) {
+    uint32_t b[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) b[j] = f_bits(__fadd_rn(__builtin_amdgcn_fmed3f(__fmul_rn(x[j], inv), -QMAX8, QMAX8), 12582912.0f));
+    uint2 o;
+    o.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
+    o.y = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[7], b[6], 0x0c0c0400u), __builtin_amdgcn_perm(b[5], b[4], 0x0c0c0400u), 0x05040100u);
+    return fine ? o : uint2{0, 0};
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_xor(v, d);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+
 // Number of the first offset past a row, E + 1 if there is none: the row is the expert's before it (the running maximum of the offsets passes
 // the row where the first offset does).  Wave-uniform; all lanes take part.
 __device__ __forceinline__ int first_offset_past(const Groups& g, const int64_t row, const int lane) {

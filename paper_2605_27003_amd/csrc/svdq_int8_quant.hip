@@ -126,11 +126,7 @@ void quantize_int8_kernel(const QuantInt8 q, const int run) {
                 top = m > top ? m : top;
             }
         }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_xor(top, d);
-            top = o > top ? o : top;
-        }
+        top = wave_max(top);
         if constexpr (W > 1) {
             if (lane == 0) part[i & 1][wave] = top;
             __syncthreads();
@@ -141,25 +137,13 @@ void quantize_int8_kernel(const QuantInt8 q, const int run) {
             }
         }
         if (!owned) continue;
-        const bool finite = top < 0x7f800000u;
-        const float rho = q.row_rho ? bits_f((uint32_t)__builtin_amdgcn_readlane((int)f_bits(ratios), i)) : q.rho;
-        float s = __fdiv_rn(__fmul_rn(rho, bits_f(top)), QMAX8);
-        const bool fine = finite && s >= 1.17549435e-38f;
-        const float inv = fine ? __fdiv_rn(1.0f, s) : 0.0f;
-        if (!fine) s = finite && s == s ? 0.0f : bits_f(0x7fc00000u);
+        float s, inv;
+        const bool fine = row_scale(top, q.row_rho ? bits_f((uint32_t)__builtin_amdgcn_readlane((int)f_bits(ratios), i)) : q.rho, s, inv);
         if (lane == 0 && tw == 0) q.sx[row] = s;
         int8_t* const out = q.qx + row * q.K;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            // clamped first, so that adding 1.5 2^23 rounds to the nearest whole number (ties to even) in the low bits
-            uint32_t b[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                b[j] = f_bits(__fadd_rn(__builtin_amdgcn_fmed3f(__fmul_rn(xs[c][j], inv), -QMAX8, QMAX8), 12582912.0f));
-            uint2 o;
-            o.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
-            o.y = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[7], b[6], 0x0c0c0400u), __builtin_amdgcn_perm(b[5], b[4], 0x0c0c0400u), 0x05040100u);
-            if (!fine) o = uint2{0, 0};
+            const uint2 o = codes8(xs[c], inv, fine);
             if (in[c]) reinterpret_cast<uint2*>(out)[at[c]] = o;
         }
     }

@@ -1,5 +1,6 @@
 """The 8-bit layer on the GPU against its definition: codes and scales from binary32 operations emulated in 64 bits, products in
 64 bits (exact: K 128^2 < 2^53)."""
+import ctypes
 import itertools
 
 import numpy as np
@@ -7,6 +8,7 @@ import pytest
 import torch
 
 import paper_2605_27003_amd as svdq
+from paper_2605_27003_amd import binding
 
 pytestmark = pytest.mark.gpu
 F32, F64, BF16, I8, I32 = torch.float32, torch.float64, torch.bfloat16, torch.int8, torch.int32
@@ -319,6 +321,40 @@ def test_layer_is_its_two_halves(M):
     assert lin.forward(x[:0], 0.8).shape == (0, N)
     none = svdq.W8A8Experts(lin.inv_lambda[None], lin.qw[None], lin.sw[None], lin.bias[None])
     assert torch.equal(none.forward(x, offsets_of([M]), 0.8), want)
+
+
+@pytest.mark.parametrize("M,N,K,E", [(1, 1, 16, 0), (1, 5120, 4096, 0), (5, 77, 144, 0), (16, 512, 512, 0), (17, 100, 528, 0), (256, 512, 512, 0), (40, 1000, 1408, 0), (33, 640, 1424, 0),
+                                     (100, 333, 2064, 0), (4, 4096, 4096, 0), (3, 200, 2992, 0), (1, 64, 64, 3), (20, 96, 272, 5), (50, 200, 1040, 40), (9, 300, 4096, 1000), (100, 128, 512, 2)])
+@pytest.mark.parametrize("gelu", [False, True])
+def test_small_layers(M, N, K, E, gelu):
+    """Layers that are one launch against the two functions, bit for bit: outputs, and the codes and scales that the C function leaves."""
+    lead = (E,) if E else ()
+    qw, sw, bias, il = codes(1, *lead, N, K), 0.001 * rand(2, *lead, N).abs(), rand(3, *lead, N), 0.5 + rand(4, *lead, K).abs()
+    tokens = max(1, M // 3) if E else M
+    x = rand(5, tokens, K + 16).to(BF16)[:, :K]
+    x[tokens // 2, K // 3] = float("nan") if M % 2 else 0.0
+    if not E:
+        want_q, want_s = svdq.quantize_act_int8(x, il, 0.8, gelu=gelu)
+        want, written = svdq.linear_w8a8(want_q, want_s, qw, sw, bias), slice(None)
+        offsets = rows = rho = None
+    else:
+        first, rho = min(2, M - 1), 0.3 + 0.7 * torch.rand(M, device="cuda")
+        offsets = offsets_of(loads_of(M, M - first, E), first)
+        rows = torch.from_numpy(np.random.default_rng(6).integers(-1, tokens + 1, M)).to(I32).cuda()
+        want_q, want_s = svdq.quantize_act_int8_grouped(x, offsets, il, rho, rows=rows, gelu=gelu)
+        want, written = svdq.linear_w8a8_grouped(want_q, want_s, offsets, qw, sw, bias), experts_of(offsets, M) >= 0
+    y, qx, sx = Guarded(M, N, BF16, ld=N + 3), Guarded(M, K, I8), Guarded(M, 1, F32)
+    layer = binding._LayerInt8(E, N, K, il.data_ptr(), qw.data_ptr(), sw.data_ptr(), bias.data_ptr())
+    at = lambda t: None if t is None else t.data_ptr()
+    rc = svdq.load_library().svdq_layer_int8_forward(ctypes.addressof(layer), x.data_ptr(), K + 16, tokens, at(rows), at(offsets), 0.8, at(rho), int(gelu), M,
+                                                     qx.t.data_ptr(), sx.t.data_ptr(), y.t.data_ptr(), N + 3, torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    same = lambda a, b, t: torch.equal(a[written].contiguous().view(t), b[written].contiguous().view(t))
+    assert same(y.t, want, torch.int16) and same(qx.t, want_q, I8) and same(sx.t[:, 0], want_s, I32)
+    assert y.intact(written) and qx.intact(written) and sx.intact(written)
+    module = svdq.W8A8Experts(il, qw, sw, bias) if E else svdq.W8A8Linear(il, qw, sw, bias)
+    got = module.forward(x, offsets, rho, rows=rows, gelu=gelu) if E else module.forward(x, 0.8, gelu=gelu)
+    assert same(got, want, torch.int16)
 
 
 def test_captured_calls_and_other_streams():
