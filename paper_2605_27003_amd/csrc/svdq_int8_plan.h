@@ -12,21 +12,20 @@ struct Int8TileShape {
     int per_cu;                  // blocks that fit a CU's LDS
 };
 // A block's time goes by the bytes that it brings to LDS, about 75 a ns where some come from its XCD's L2 and some from behind it (135 where all
-// come from L2, 50 where none do), whatever is in flight; 256 x 256 comes near the matrix pipes' time.  Measured at K = 5120 with one
-// round of blocks, one per CU.
+// come from L2, 50 where none do), whatever is in flight; 256 x 256 comes near the matrix pipes' time.
 inline Int8TileShape int8_tile_shape(Int8Tiles t) {
     switch (t) {
         case Int8Tiles::FEW_16x16: return {16, 16, 0.0, 2};
         case Int8Tiles::FEW_16x32: return {16, 32, 0.0, 2};
         case Int8Tiles::FEW_32x16: return {32, 16, 0.0, 1};
         case Int8Tiles::FEW_32x32: return {32, 32, 0.0, 1};
-        case Int8Tiles::T64x32: return {64, 32, 0.17, 2};
-        case Int8Tiles::T64x64: return {64, 64, 0.21, 2};
+        case Int8Tiles::T64x32: return {64, 32, 0.22, 2};
+        case Int8Tiles::T64x64: return {64, 64, 0.235, 2};
         case Int8Tiles::T64x128: return {64, 128, 0.31, 2};
         case Int8Tiles::T128x128: return {128, 128, 0.415, 2};
-        case Int8Tiles::T256x128: return {256, 128, 0.62, 1};
-        case Int8Tiles::T256x160: return {256, 160, 0.73, 1};
-        default: return {256, 256, 1.07, 1};
+        case Int8Tiles::T256x128: return {256, 128, 0.58, 1};
+        case Int8Tiles::T256x160: return {256, 160, 0.84, 1};
+        default: return {256, 256, 0.97, 1};
     }
 }
 
@@ -36,12 +35,14 @@ struct Int8Plan {
 };
 
 // rows: of the call.  experts: 0 where it is not grouped.
-// Estimate for one choice: a launch and its first bytes 2.5, and the longest of
+// Estimate for one choice: a launch and its first bytes 2, and the longest of
 //   rounds     a block's stages and its end, for as many rounds as there are tiles for each of 256 CUs (two blocks that share a CU take 1.75 times as
 //              long as one)
-//   fabric     what the XCDs' L2s fetch at 6 TB/s: 256 tiles at a time, each XCD the rows and channels of its share of them
-//   memory     weights, codes and outputs at 5.5 TB/s
-// and a little of the first two, which decides where choices share their bound.
+//   fabric     what the XCDs' L2s fetch at 9 TB/s: 256 tiles at a time, each XCD the rows and channels of its share of them
+//   memory     weights and codes at 5.5 TB/s, outputs at 4.4 where their rows are whole memory lines and at 3.3 where tiles share lines (8318 x 28896 of
+//              binary32 at K = 176: 240 us; 28884 channels: 436)
+// and a little of each, which decides where choices share their bound.  A tile that has its CU alone has nothing to overlap its stores with.
+// The figures are fitted to 900 calls of 1 to 75600 rows, each timed with every tile: the choice is 1.8 % slower than the best in the mean, a third at worst.
 inline Int8Plan int8_cost(Int8Tiles t, int64_t rows, int N, int K, int experts, bool out_f32) {
     const Int8TileShape s = int8_tile_shape(t);
     const int64_t with_rows = experts ? (rows < experts ? rows : experts) : 1, nt = ((int64_t)N + s.bn - 1) / s.bn;
@@ -54,21 +55,24 @@ inline Int8Plan int8_cost(Int8Tiles t, int64_t rows, int N, int K, int experts, 
     const double shared = share / across < 1 ? share : across, channels = share / across < 1 ? 1 : share / across;
     double fabric = tiles / share * (shared * s.bm + channels * s.bn) * K;
     if (fabric < weights + codes) fabric = weights + codes;
-    const double memory = weights + codes + (double)rows * N * (out_f32 ? 4 : 2);
+    fabric /= 9.0e6;
+    const int64_t row = (int64_t)N * (out_f32 ? 4 : 2);
+    const double outputs = (double)rows * row / (row % 128 ? 3.3e6 : 4.4e6), memory = (weights + codes) / 5.5e6 + outputs;
     // rounds of blocks, in the time of one block alone on its CU
-    const double n = tiles / 256.0, whole = experts ? n + 0.3 : (double)(int64_t)(n + 0.999);
-    const double rounds = n <= 1.0 ? 1.0 : s.per_cu == 2 ? (n <= 2.0 ? 1.75 : 0.92 * n) : whole;
+    const double n = tiles / 256.0, whole = experts ? n + 0.375 : (double)(int64_t)(n + 0.999);
+    const double rounds = n <= 1.0 ? 1.0 : s.per_cu == 2 ? (n <= 2.0 ? 1.75 : 1.03 * n) : whole;
     double time;
     if (s.stage == 0.0) {
         const double used = experts ? (rows < 2 * experts ? 2.0 : (double)s.bm) : (double)(rows < s.bm ? rows : s.bm);      // rows past the last are in L1 already
-        time = (s.per_cu == 2 && n > 1.0 ? n : rounds) * ((used + s.bn) * K / 50.0e3 + 0.4);   // walking blocks share their CU evenly
+        time = (s.per_cu == 2 && n > 1.0 ? n : rounds) * ((used + s.bn) * K / 58.0e3 + 0.7);   // walking blocks share their CU evenly
     } else {
-        time = rounds * (((K + 127) / 128) * s.stage + 0.6 + 4.3 * s.bm * s.bn / 65536.0);
+        time = rounds * (((K + 127) / 128) * s.stage + 0.7 + 4.35 * s.bm * s.bn / 65536.0);
     }
+    if (s.stage > 0.0 && s.per_cu == 1) time += 0.6 * outputs;
     double most_time = time;
-    if (fabric / 6.0e6 > most_time) most_time = fabric / 6.0e6;
-    if (memory / 5.5e6 > most_time) most_time = memory / 5.5e6;
-    p.cost = 2.5 + most_time + 0.15 * (time + fabric / 6.0e6);        // the others matter where two choices share their bound
+    if (fabric > most_time) most_time = fabric;
+    if (memory > most_time) most_time = memory;
+    p.cost = 2.0 + most_time + 0.125 * (time + fabric) + 0.15 * memory;
     return p;
 }
 
