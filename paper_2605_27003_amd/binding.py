@@ -835,14 +835,15 @@ class _W8A8:
         self._descriptor()
 
     def _descriptor(self):
-        """svdq_layer_int8 of the tensors that the layer holds now, checked when they have changed.  The caller keeps it through
-        its call."""
+        """svdq_layer_int8 of the tensors that the layer holds now, checked when they, or the memory that they have, have changed.
+        The caller keeps it through its call."""
+        inv_lambda, qw, sw, bias = tensors = self.inv_lambda, self.qw, self.sw, self.bias
+        at = (None if inv_lambda is None else inv_lambda.data_ptr(), qw.data_ptr(), sw.data_ptr(), None if bias is None else bias.data_ptr())
         held = self._held
         if held is not None:
-            a, b, c, d = held[0]
-            if a is self.inv_lambda and b is self.qw and c is self.sw and d is self.bias:
-                return held[1]
-        inv_lambda, qw, sw, bias = tensors = self.inv_lambda, self.qw, self.sw, self.bias
+            (a, b, c, d), was, layer = held
+            if a is inv_lambda and b is qw and c is sw and d is bias and at == was:
+                return layer
         if qw.dim() != 2 + self.GROUPED:
             raise ValueError(f"qw: {'[E, N, K]' if self.GROUPED else '[N, K]'} is needed, not {tuple(qw.shape)}")
         lead, (N, K), gpu = tuple(qw.shape[:-2]), qw.shape[-2:], qw.get_device()
@@ -850,7 +851,7 @@ class _W8A8:
                            _tensor("qw", qw, _I8, lead + (N, K), gpu), _tensor("sw", sw, _F32, lead + (N,), gpu),
                            None if bias is None else _tensor("bias", bias, _F32, lead + (N,), gpu))
         layer.address, layer.shape = ctypes.addressof(layer), (layer.E, N, K, gpu)
-        self._held = (tensors, layer)
+        self._held = (tensors, at, layer)
         return layer
 
     def __getstate__(self):

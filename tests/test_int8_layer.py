@@ -93,3 +93,17 @@ def test_the_layers_descriptor_follows_its_tensors():
     lin.sw = torch.ones(9)
     with pytest.raises(ValueError):
         lin._descriptor()
+
+
+def test_descriptor_follows_memory_given_to_the_same_tensor():
+    qw, sw, bias, il = torch.zeros((32, 48), dtype=torch.int8), torch.ones(32), torch.ones(32), torch.ones(48)
+    layer = svdq.W8A8Linear(il, qw, sw, bias)
+    first = layer._descriptor()
+    assert layer._descriptor() is first and first.qw == qw.data_ptr()
+    for name in ("inv_lambda", "qw", "sw", "bias"):
+        held = getattr(layer, name)
+        held.data = held.clone()
+        assert getattr(layer._descriptor(), name) == held.data_ptr()
+    layer.qw.data = torch.zeros((32, 64), dtype=torch.int8)
+    with pytest.raises(ValueError, match="inv_lambda"):
+        layer._descriptor()
