@@ -1,13 +1,14 @@
 // The product of the 8-bit layer on the int8 matrix cores: y = (qx qw^T) sx sw + bias, 32-bit integer sums over all of K (exact
 // for every K the interface takes: K 127^2 < 2^31), then three binary32 operations and one rounding to the output's type.
 //
-// v_mfma_i32_32x32x32_i8: lane l holds row l % 32 of its operand and the 16 consecutive k [16 (l / 32), +16) as 16 bytes.  As in the
-// 4-bit kernels the transposed tile D[n][m] is computed (weights are the A operand), so that a lane owns one token and, per
-// register quad, four consecutive channels.
+// v_mfma_i32_16x16x64_i8: lane l holds row l % 16 of its operand and the 16 consecutive k [16 (l / 16), +16) as 16 bytes.  As in the
+// 4-bit kernels the transposed tile D[n][m] is computed (weights are the A operand), so that a lane owns token l % 16 and the four
+// consecutive channels from 4 (l / 16) on.  (The 32 x 32 x 32 instruction halves the operand reads, but
+// 32760 x 5120 x 13824 ran at 2.62 POP/s with it against 2.83.)
 //
 // Both operands lie in memory as they come, rows of K bytes.  A stage is 128 k of every row of the tile, one full memory line per
 // row: eight lanes of a direct global->LDS transfer move a row's line, and since lane i's 16 bytes land at LDS place i the
-// lanes pick their pieces in rotated order: piece c of row r stands at place c ^ ((r / 2) % 8) of its 128 bytes.  The 32 rows
+// lanes pick their pieces in rotated order: piece c of row r stands at place c ^ ((r / 2) % 8) of its 128 bytes.  The 16 rows
 // that an operand read covers then meet all banks evenly.
 #include "svdq_int8_dev.h"
 #include "svdq_int8_plan.h"
@@ -16,25 +17,13 @@ namespace svdq {
 
 namespace {
 
-// The matrix instruction of a kernel: I x I results of 1024 / I k.  Lane l holds row l % I of an operand and 16 consecutive k (bytes), those
-// from 16 (l / I) on; of the results it holds column (token) l % I and QUADS runs of four rows (channels), the first at 4 (l / I), 8 apart.
-template <int I> struct Mfma;
-template <> struct Mfma<32> {
-    using Acc = int16v;
-    static constexpr int QUADS = 4;
-    static __device__ __forceinline__ Acc mul(int4v a, int4v b, Acc c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
-};
-template <> struct Mfma<16> {
-    using Acc = int4v;
-    static constexpr int QUADS = 1;
-    static __device__ __forceinline__ Acc mul(int4v a, int4v b, Acc c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
-};
+constexpr int I = 16;            // tokens, and channels, of a matrix instruction
 
 // The end of a tile whose scales and biases stand in LDS (binary32: the tokens', the channels', the channels' biases): y = acc sx sw + bias,
 // up to MOST tokens at a time in column groups whose rows are one memory line (128 bytes) where the wave has as many channels, each
 // transposed through the wave's own LDS and stored `unit` bytes a lane, as the rows' alignment allows: 16 (a piece over the last channel goes
 // element by element), 4, or an element.
-template <class T, int I, int MT, int NT, int MOST>
+template <class T, int MT, int NT, int MOST>
 struct TileStore {
     static constexpr int EL = 16 / (int)sizeof(T), LINE = 8 * EL / I;  // blocks of a line
     static constexpr int CB = NT % LINE == 0 ? LINE : NT % 2 == 0 && LINE > 2 ? 2 : 1, COLS = CB * I, ROWS = MT * I <= MOST ? MT * I : MOST;
@@ -42,7 +31,7 @@ struct TileStore {
     static constexpr int MP = ROWS / I, LANES = COLS / EL, STEP = 64 / LANES;
     static_assert(NT % CB == 0 && MT % MP == 0, "whole groups");
     // region: BYTES of the wave's own.  tokens, channels, biases: LDS addresses of the wave's first.
-    static __device__ __forceinline__ void run(const typename Mfma<I>::Acc (&acc)[NT][MT], const uint32_t region, const uint32_t tokens, const uint32_t channels, const uint32_t biases,
+    static __device__ __forceinline__ void run(const int4v (&acc)[NT][MT], const uint32_t region, const uint32_t tokens, const uint32_t channels, const uint32_t biases,
                                                const bool has_bias, const int lane, T* __restrict__ y, const int64_t ldy, const int rows, const int cols, const int unit) {
         const int li = lane % I, lk = lane / I;
 #pragma unroll
@@ -53,28 +42,26 @@ struct TileStore {
 #pragma unroll
             for (int g = 0; g < NT / CB; ++g) {
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb)
+                for (int cb = 0; cb < CB; ++cb) {
+                    const int ni = g * CB + cb, at = 4 * lk;
+                    const uint32_t c = (ni * I + at) * 4;
+                    const uint4 s4 = lds_read16(channels + c), b4 = has_bias ? lds_read16(biases + c) : uint4{0, 0, 0, 0};
+                    const float s[4] = {bits_f(s4.x), bits_f(s4.y), bits_f(s4.z), bits_f(s4.w)};
+                    const float b[4] = {bits_f(b4.x), bits_f(b4.y), bits_f(b4.z), bits_f(b4.w)};
 #pragma unroll
-                    for (int q = 0; q < Mfma<I>::QUADS; ++q) {
-                        const int ni = g * CB + cb, at = 8 * q + 4 * lk;
-                        const uint32_t c = (ni * I + at) * 4;
-                        const uint4 s4 = lds_read16(channels + c), b4 = has_bias ? lds_read16(biases + c) : uint4{0, 0, 0, 0};
-                        const float s[4] = {bits_f(s4.x), bits_f(s4.y), bits_f(s4.z), bits_f(s4.w)};
-                        const float b[4] = {bits_f(b4.x), bits_f(b4.y), bits_f(b4.z), bits_f(b4.w)};
+                    for (int mi = 0; mi < MP; ++mi) {
+                        float v[4];
 #pragma unroll
-                        for (int mi = 0; mi < MP; ++mi) {
-                            float v[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) v[i] = ((float)acc[ni][m0 + mi][4 * q + i] * ts[mi]) * s[i] + b[i];
-                            const uint32_t to = region + (mi * I + li) * PITCH + (cb * I + at) * (int)sizeof(T);
-                            if constexpr (sizeof(T) == 2) {
-                                lds_write8_pinned(to, uint2{f2_bf16_rne(v[0], v[1]), f2_bf16_rne(v[2], v[3])});
-                            } else {
-                                lds_write8_pinned(to, uint2{f_bits(v[0]), f_bits(v[1])});
-                                lds_write8_pinned(to + 8, uint2{f_bits(v[2]), f_bits(v[3])});
-                            }
+                        for (int i = 0; i < 4; ++i) v[i] = ((float)acc[ni][m0 + mi][i] * ts[mi]) * s[i] + b[i];
+                        const uint32_t to = region + (mi * I + li) * PITCH + (cb * I + at) * (int)sizeof(T);
+                        if constexpr (sizeof(T) == 2) {
+                            lds_write8_pinned(to, uint2{f2_bf16_rne(v[0], v[1]), f2_bf16_rne(v[2], v[3])});
+                        } else {
+                            lds_write8_pinned(to, uint2{f_bits(v[0]), f_bits(v[1])});
+                            lds_write8_pinned(to + 8, uint2{f_bits(v[2]), f_bits(v[3])});
                         }
                     }
+                }
                 __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
                 __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
                 const int left = cols - g * COLS;
@@ -133,7 +120,7 @@ struct TileStore {
 // A tile of BM tokens by BN channels for WM x WN waves; its operands stand in LDS from DEPTH stages ahead on.
 template <int BM_, int BN_, int WM_, int WN_, int DEPTH_>
 struct Int8Tile {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, DEPTH = DEPTH_, I = 16, NW = WM * WN, THREADS = 64 * NW, MT = BM / WM / I, NT = BN / WN / I;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, DEPTH = DEPTH_, NW = WM * WN, THREADS = 64 * NW, MT = BM / WM / I, NT = BN / WN / I;
     static constexpr int NA = (BM / 8 + NW - 1) / NW, NB = (BN / 8 + NW - 1) / NW;                    // transfers of a wave a stage, eight rows each
     static constexpr uint32_t A = BM * BK, W = BN * BK, RING = (DEPTH + 1) * A + DEPTH * W;
     static constexpr int TOKENS = (BM + 63) / 64 * 64, CHANNELS = (BN + 63) / 64 * 64;                // scales and biases come 64 at a time
@@ -149,9 +136,8 @@ struct Int8Tile {
 template <class G, bool TAIL, bool GROUPED, class T>
 __global__ __launch_bounds__(G::THREADS, 1)
 void gemm_int8_kernel(const GemmInt8 g) {
-    constexpr int BM = G::BM, BN = G::BN, MT = G::MT, NT = G::NT, NA = G::NA, NB = G::NB, I = G::I, DEPTH = G::DEPTH;
-    using Acc = typename Mfma<I>::Acc;
-    using Store = TileStore<T, I, MT, NT, (G::RING >= (G::NW + 1) * 64 * 144 + G::SCALES ? 64 : 32)>;
+    constexpr int BM = G::BM, BN = G::BN, MT = G::MT, NT = G::NT, NA = G::NA, NB = G::NB, DEPTH = G::DEPTH;
+    using Store = TileStore<T, MT, NT, (G::RING >= (G::NW + 1) * 64 * 144 + G::SCALES ? 64 : 32)>;
     static_assert(G::RING >= (G::NW + 1) * Store::BYTES + G::SCALES && G::A >= G::SCALES, "the store transposes in the ring, beside the scales");
     __shared__ __attribute__((aligned(16))) uint8_t ring[G::RING];
 
@@ -222,11 +208,11 @@ void gemm_int8_kernel(const GemmInt8 g) {
         }
     };
 
-    Acc acc[NT][MT];
+    int4v acc[NT][MT];
 #pragma unroll
     for (int ni = 0; ni < NT; ++ni)
 #pragma unroll
-        for (int mi = 0; mi < MT; ++mi) acc[ni][mi] = (Acc)(0);
+        for (int mi = 0; mi < MT; ++mi) acc[ni][mi] = int4v{0, 0, 0, 0};
 
     uint32_t cur_a = ring_a, cur_w = ring_w;
 #pragma unroll
@@ -267,7 +253,7 @@ void gemm_int8_kernel(const GemmInt8 g) {
 #pragma unroll
             for (int n = from; n < until; ++n) {
                 const int t = n % T_, ni = t / MT, mi = t % MT;
-                acc[ni][mi] = Mfma<I>::mul(op[kk & 1].w[ni], op[kk & 1].x[mi], acc[ni][mi]);
+                acc[ni][mi] = __builtin_amdgcn_mfma_i32_16x16x64_i8(op[kk & 1].w[ni], op[kk & 1].x[mi], acc[ni][mi], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
                 if (!(next && last) && n >= r0)
 #pragma unroll
