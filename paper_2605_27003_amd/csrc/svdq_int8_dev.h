@@ -162,10 +162,12 @@ struct GroupTiles {
 template <bool GROUPED, int BM, int BN> struct TilesOf { using type = DenseTiles<BM, BN>; };
 template <int BM, int BN> struct TilesOf<true, BM, BN> { using type = GroupTiles<BM, BN>; };
 
-// As many blocks as there can be tiles: every expert with rows adds at most one row tile that is not full.
-inline int most_tiles(const GemmInt8& g, const int bm, const int bn) {
+// Every expert with rows adds at most one row tile that is not full.
+inline int64_t tiles_there_can_be(const GemmInt8& g, const int bm, const int bn) {
     const int64_t mt = g.groups.offsets ? g.M / bm + (g.M < g.groups.E ? g.M : g.groups.E) : (g.M + bm - 1) / bm;
-    return (int)((mt * ((g.N + bn - 1) / bn) + 255) / 256 * 256);
+    return mt * (((int64_t)g.N + bn - 1) / bn);
 }
+// As many blocks.
+inline int most_tiles(const GemmInt8& g, const int bm, const int bn) { return (int)((tiles_there_can_be(g, bm, bn) + 255) / 256 * 256); }
 
 }  // namespace svdq

@@ -118,8 +118,9 @@ struct TileStore {
 };
 
 // A tile of BM tokens by BN channels for WM x WN waves; its operands stand in LDS from DEPTH stages ahead on.
-template <int BM_, int BN_, int WM_, int WN_, int DEPTH_>
+template <int BM_, int BN_, int WM_, int WN_, int DEPTH_, bool LINES_ = false>
 struct Int8Tile {
+    static constexpr bool LINES = LINES_;                             // fetched by whole lines: of a K that is no multiple of a stage
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, DEPTH = DEPTH_, NW = WM * WN, THREADS = 64 * NW, MT = BM / WM / I, NT = BN / WN / I;
     static constexpr int NA = (BM / 8 + NW - 1) / NW, NB = (BN / 8 + NW - 1) / NW;                    // transfers of a wave a stage, eight rows each
     static constexpr uint32_t A = BM * BK, W = BN * BK, RING = (DEPTH + 1) * A + DEPTH * W;
@@ -133,13 +134,21 @@ struct Int8Tile {
 // last, where W(s) stood: requests that come all at once behind the barrier take longer than the instructions that they stand between
 // (with a place less and all of them there, 256 x 256 tiles took 6 % longer at K = 13824).
 // TAIL: K is no multiple of a stage.  The last stage's pieces beyond K repeat the row's last piece, and count as zeros in the weights' operand.
+//
+// LINES: rows of such a K begin anywhere in a memory line, so that 128 bytes from where a row begins are parts of two lines and a stage's transfers
+// fetch every line twice.  Here they fetch whole lines: window j of a row is the j-th line that the row has a part of, its k begin `phase`
+// pieces into window 0, and stage s reads windows s and s + 1, each lane the one that its piece is in.  (The phase of a row goes by its number modulo
+// 16, so that a lane has one for all its rows; the rotation above still spreads 16 rows over all banks, for every K.)  A stage more has to have
+// arrived, and the channels' ring has a place more: tiles of up to 128 tokens have the LDS.  512 x 5120, K = 5136: 21.2 us, 27.5 without.
 template <class G, bool TAIL, bool GROUPED, class T>
 __global__ __launch_bounds__(G::THREADS, 1)
 void gemm_int8_kernel(const GemmInt8 g) {
     constexpr int BM = G::BM, BN = G::BN, MT = G::MT, NT = G::NT, NA = G::NA, NB = G::NB, DEPTH = G::DEPTH;
-    using Store = TileStore<T, MT, NT, (G::RING >= (G::NW + 1) * 64 * 144 + G::SCALES ? 64 : 32)>;
-    static_assert(G::RING >= (G::NW + 1) * Store::BYTES + G::SCALES && G::A >= G::SCALES, "the store transposes in the ring, beside the scales");
-    __shared__ __attribute__((aligned(16))) uint8_t ring[G::RING];
+    constexpr bool LINES = TAIL && G::LINES;
+    constexpr uint32_t RING = G::RING + (LINES ? G::W : 0);
+    using Store = TileStore<T, MT, NT, (RING >= (G::NW + 1) * 64 * 144 + G::SCALES ? 64 : 32)>;
+    static_assert(RING >= (G::NW + 1) * Store::BYTES + G::SCALES && G::A >= G::SCALES, "the store transposes in the ring, beside the scales");
+    __shared__ __attribute__((aligned(16))) uint8_t ring[RING];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -159,37 +168,45 @@ void gemm_int8_kernel(const GemmInt8 g) {
     const int8_t* const abase = g.qx + (int64_t)m0 * K;
     const int8_t* const wbase = at.qw + (int64_t)n0 * K;
     const int place = lane & 7;
-    uint32_t va[NA], vw[NB], pa[NA], pw[NB];
-    auto rows_of = [&](uint32_t& v, uint32_t& piece, const int block, const int last) {              // rows past the end repeat the last one
-        const int row = 8 * block + (lane >> 3);
-        piece = place ^ ((row >> 1) & 7);
-        v = (uint32_t)(row < last ? row : last) * (uint32_t)K + piece * 16;
+    const uint32_t first_a = (uint32_t)((uintptr_t)abase >> 4), first_w = (uint32_t)((uintptr_t)wbase >> 4);
+    auto phase = [&](const uint32_t first, const int row) { return LINES ? (int)((first + (uint32_t)row * (uint32_t)(K >> 4)) & 7) : 0; };
+    uint32_t va[NA], vw[NB];
+    int pa[NA], pw[NB];                                               // piece of a row in stage 0: negative ones are the row's before
+    auto rows_of = [&](uint32_t& v, int& piece, const uint32_t first, const int block, const int last) {      // rows past the end repeat the last one
+        const int row = 8 * block + (lane >> 3), from = row < last ? row : last;
+        piece = (place ^ ((row >> 1) & 7)) - phase(first, from);
+        v = (uint32_t)from * (uint32_t)K + (uint32_t)(piece + (LINES ? 8 : 0)) * 16;
     };
 #pragma unroll
-    for (int j = 0; j < NA; ++j) rows_of(va[j], pa[j], block_a(j), m_end - 1 - m0);
+    for (int j = 0; j < NA; ++j) rows_of(va[j], pa[j], first_a, block_a(j), m_end - 1 - m0);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) rows_of(vw[j], pw[j], block_w(j), N - 1 - n0);
-    // EDGE: of what may be the last stage, whose pieces can lie beyond K
-    auto request = [&](auto EDGEC, const int8_t* base, uint32_t v, const uint32_t piece, const int s, const uint32_t to) {
+    for (int j = 0; j < NB; ++j) rows_of(vw[j], pw[j], first_w, block_w(j), N - 1 - n0);
+    // EDGE: of what may be the last stage (with LINES, one of the last two windows or the first), whose pieces can lie beyond K (or before the row)
+    auto request = [&](auto EDGEC, const int8_t* base, uint32_t v, const int piece, const int s, const uint32_t to) {
         if constexpr (TAIL && decltype(EDGEC)::value) {
-            const int left = (K >> 4) - 8 * s - 1, over = (int)piece - left;
-            if (over > 0) v -= over * 16;
+            const int k16 = 8 * s + piece, last = (K >> 4) - 1;
+            if (k16 > last) v -= (k16 - last) * 16;
+            if (LINES && k16 < 0) v -= k16 * 16;
         }
-        dma16(base + (int64_t)s * BK, v, to);
+        dma16(base + (int64_t)(s - (LINES ? 1 : 0)) * BK, v, to);
     };
     auto request_a = [&](auto EDGEC, const int s, const uint32_t to, const int j) { request(EDGEC, abase, va[j], pa[j], s, to + block_a(j) * 1024); };
     auto request_w = [&](auto EDGEC, const int s, const uint32_t to, const int j) { request(EDGEC, wbase, vw[j], pw[j], s, to + block_w(j) * 1024); };
     auto next_a = [&](const uint32_t c) { return c == ring_a + DEPTH * G::A ? ring_a : c + G::A; };
-    auto next_w = [&](const uint32_t c) { return c == ring_w + (DEPTH - 1) * G::W ? ring_w : c + G::W; };
+    constexpr int PLACES_W = LINES ? DEPTH + 1 : DEPTH;
+    auto next_w = [&](const uint32_t c) { return c == ring_w + (PLACES_W - 1) * G::W ? ring_w : c + G::W; };
 
     // ---- operands: piece PS kk + lk of a row, for k step kk, stands at that place ^ (row / 2) % 8
     constexpr int PS = 64 / I, STEPS = 8 / PS;
-    const uint32_t turn = (lk ^ (li >> 1)) & 7;
+    const int turn = (li >> 1) & 7;
     uint32_t rd_a[STEPS], rd_w[STEPS];
+    bool on_a[STEPS], on_w[STEPS];                                    // the lane's piece is in the window behind
 #pragma unroll
     for (int kk = 0; kk < STEPS; ++kk) {
-        rd_a[kk] = (wm * MT * I + li) * BK + ((turn ^ (PS * kk)) << 4);
-        rd_w[kk] = (wn * NT * I + li) * BK + ((turn ^ (PS * kk)) << 4);
+        const int qa = PS * kk + lk + phase(first_a, li), qw = PS * kk + lk + phase(first_w, li);
+        rd_a[kk] = (wm * MT * I + li) * BK + (((qa & 7) ^ turn) << 4);
+        rd_w[kk] = (wn * NT * I + li) * BK + (((qw & 7) ^ turn) << 4);
+        on_a[kk] = LINES && qa > 7, on_w[kk] = LINES && qw > 7;
     }
     struct Operands {
         int4v w[NT], x[MT];
@@ -215,9 +232,10 @@ void gemm_int8_kernel(const GemmInt8 g) {
         for (int mi = 0; mi < MT; ++mi) acc[ni][mi] = int4v{0, 0, 0, 0};
 
     uint32_t cur_a = ring_a, cur_w = ring_w;
+    const int windows = nstages + (LINES ? 1 : 0);                    // of the transfers
 #pragma unroll
     for (int s = 0; s < DEPTH; ++s)
-        if (s < nstages) {
+        if (s < windows) {
 #pragma unroll
             for (int j = 0; j < NA; ++j) request_a(IC<1>{}, s, ring_a + s * G::A, j);
 #pragma unroll
@@ -230,13 +248,13 @@ void gemm_int8_kernel(const GemmInt8 g) {
         else if (behind == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NA + NB) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
-    static_assert(DEPTH <= 4, "wait_for");
-    wait_for((nstages < DEPTH ? nstages : DEPTH) - 1);
+    static_assert(DEPTH <= 4 && (!LINES || DEPTH >= 3), "the waits");
+    wait_for((windows < DEPTH ? windows : DEPTH) - (LINES ? 2 : 1));
     __syncthreads();
     constexpr int T_ = MT * NT, READS = MT + NT, QUARTER = STEPS * T_ / 4;
     Operands op[2];
 #pragma unroll
-    for (int r = 0; r < READS; ++r) read(IC<1>{}, op[0], ring_a + rd_a[0], ring_w + rd_w[0], 0, 0, r);
+    for (int r = 0; r < READS; ++r) read(IC<1>{}, op[0], (on_a[0] ? ring_a + G::A : ring_a) + rd_a[0], (on_w[0] ? ring_w + G::W : ring_w) + rd_w[0], 0, 0, r);
 
     // A stage is STEPS k steps, of T_ instructions each; between those the reads of the next step's operands and the stage's requests.
     // Before its last quarter (when every wave has all of its operands) stand the wait for the next stage's rows and the barrier.
@@ -244,11 +262,15 @@ void gemm_int8_kernel(const GemmInt8 g) {
     auto stage = [&](const int s, auto FILLC, auto EDGEC, auto LASTC) {
         constexpr bool fill = decltype(FILLC)::value, last = decltype(LASTC)::value;
         const uint32_t na = next_a(cur_a), nw = next_w(cur_w), free_a = cur_a == ring_a ? ring_a + DEPTH * G::A : cur_a - G::A;
+        const uint32_t free_w = !LINES ? cur_w : cur_w == ring_w ? ring_w + DEPTH * G::W : cur_w - G::W;
         auto instructions = [&](auto FROM, auto TO) {
             constexpr int from = decltype(FROM)::value, until = decltype(TO)::value, kk = from / T_, rk = (kk + 1) % STEPS;
             constexpr bool next = kk + 1 == STEPS;                    // its reads are of the next stage, behind the barrier
             constexpr int r0 = next ? 3 * QUARTER : kk * T_, span = next ? QUARTER : T_, RP = (READS + span - 1) / span;
-            uint32_t fa = (next ? na : cur_a) + rd_a[rk], fw = (next ? nw : cur_w) + rd_w[rk];
+            uint32_t fa = next ? na : cur_a, fw = next ? nw : cur_w;
+            if constexpr (LINES) fa = on_a[rk] ? next_a(fa) : fa, fw = on_w[rk] ? next_w(fw) : fw;
+            fa += rd_a[rk];
+            fw += rd_w[rk];
             asm volatile("" : "+v"(fa), "+v"(fw));
 #pragma unroll
             for (int n = from; n < until; ++n) {
@@ -265,14 +287,14 @@ void gemm_int8_kernel(const GemmInt8 g) {
                         if (n == (2 * j + 1) * 3 * QUARTER / (2 * NA)) request_a(EDGEC, s + DEPTH, free_a, j);
 #pragma unroll
                     for (int j = 0; j < NB; ++j)
-                        if (n == 3 * QUARTER + j * QUARTER / NB) request_w(EDGEC, s + DEPTH, cur_w, j);
+                        if (n == 3 * QUARTER + j * QUARTER / NB) request_w(EDGEC, s + DEPTH, free_w, j);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
         instructions(IC<0>{}, IC<T_>{});
         instructions(IC<T_>{}, IC<3 * QUARTER>{});
-        if constexpr (fill) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 2) * (NA + NB) + NA) : "memory");
+        if constexpr (fill) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - (LINES ? 3 : 2)) * (NA + NB) + NA) : "memory");
         else wait_for(nstages - 2 - s);
         __syncthreads();
         instructions(IC<3 * QUARTER>{}, IC<4 * QUARTER>{});
@@ -280,11 +302,12 @@ void gemm_int8_kernel(const GemmInt8 g) {
         cur_w = nw;
     };
     int s = 0;
-    for (; s + DEPTH + (TAIL ? 1 : 0) < nstages; ++s) stage(s, IC<1>{}, IC<0>{}, IC<0>{});
-    if (TAIL && s + DEPTH < nstages) stage(s++, IC<1>{}, IC<1>{}, IC<0>{});
+    for (; s + DEPTH + (LINES ? 2 : TAIL ? 1 : 0) < windows; ++s) stage(s, IC<1>{}, IC<0>{}, IC<0>{});
+    if constexpr (TAIL)
+        for (; s + DEPTH < windows; ++s) stage(s, IC<1>{}, IC<1>{}, IC<0>{});
     for (; s + 1 < nstages; ++s) stage(s, IC<0>{}, IC<1>{}, IC<0>{});
-    // the last stage's requests are the tile's scales and biases, 64 values each, into the place behind its tokens'
-    const uint32_t scales = next_a(cur_a);
+    // the last stage's requests are the tile's scales and biases, 64 values each, into a free place of the tokens'
+    const uint32_t scales = LINES ? (cur_a == ring_a ? ring_a + DEPTH * G::A : cur_a - G::A) : next_a(cur_a);
     for (int j = wave; j < (int)G::SCALES / 256; j += G::NW) {
         constexpr int CHANNEL0 = G::TOKENS / 64, BIAS0 = CHANNEL0 + G::CHANNELS / 64;
         const bool tok = j < CHANNEL0, bia = j >= BIAS0;
@@ -312,20 +335,28 @@ hipError_t launch_tiles(const GemmInt8& g, const bool out_f32, hipStream_t strea
         else go(gemm_int8_kernel<G, TAIL, GROUPED, uint16_t>);
     };
     const bool grouped = g.groups.offsets != nullptr;
-    if (g.K % BK) grouped ? typed(IC<1>{}, IC<1>{}) : typed(IC<1>{}, IC<0>{});
-    else grouped ? typed(IC<0>{}, IC<1>{}) : typed(IC<0>{}, IC<0>{});
+    if (G::LINES || g.K % BK) grouped ? typed(IC<1>{}, IC<1>{}) : typed(IC<1>{}, IC<0>{});
+    else if constexpr (!G::LINES) grouped ? typed(IC<0>{}, IC<1>{}) : typed(IC<0>{}, IC<0>{});
     return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_gemm_int8(const GemmInt8& g, const Int8Plan& p, bool out_f32, hipStream_t stream) {
+    const Int8TileShape shape = int8_tile_shape(p.tiles);
+    const int64_t tiles = tiles_there_can_be(g, shape.bm, shape.bn);
+    // rows fetched by whole lines, a block alone on its CU: where enough blocks share what L2 gives.  (Few wait for latency, and have less under way so:
+    // one tile of 128 x 128 takes up to 1.29 times as long, 48 to 256 tiles 0.7 to 1.1 times, 0.94 in the mean of 80 products.)
+    const bool lines = g.K % BK && tiles > 48 && tiles <= 256;
     switch (p.tiles) {
         case Int8Tiles::T64x32: return launch_tiles<Int8Tile<64, 32, 2, 2, 4>>(g, out_f32, stream);
         case Int8Tiles::T64x64: return launch_tiles<Int8Tile<64, 64, 2, 2, 4>>(g, out_f32, stream);
-        case Int8Tiles::T64x128: return launch_tiles<Int8Tile<64, 128, 2, 4, 3>>(g, out_f32, stream);
+        case Int8Tiles::T64x128:
+            if (lines) return launch_tiles<Int8Tile<64, 128, 2, 4, 4, true>>(g, out_f32, stream);
+            return launch_tiles<Int8Tile<64, 128, 2, 4, 3>>(g, out_f32, stream);
         case Int8Tiles::T128x128:                                     // a block alone on its CU, or two
-            if (most_tiles(g, 128, 128) <= 256) return launch_tiles<Int8Tile<128, 128, 2, 4, 4>>(g, out_f32, stream);
+            if (lines) return launch_tiles<Int8Tile<128, 128, 2, 4, 4, true>>(g, out_f32, stream);
+            if (tiles <= 256) return launch_tiles<Int8Tile<128, 128, 2, 4, 4>>(g, out_f32, stream);
             return launch_tiles<Int8Tile<128, 128, 2, 4, 2>>(g, out_f32, stream);
         case Int8Tiles::T256x128: return launch_tiles<Int8Tile<256, 128, 4, 2, 2>>(g, out_f32, stream);
         case Int8Tiles::T256x160: return launch_tiles<Int8Tile<256, 160, 4, 2, 2>>(g, out_f32, stream);

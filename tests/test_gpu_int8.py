@@ -420,3 +420,17 @@ def test_addresses_beyond_32_bits():
     big[-5:] = x
     rows = torch.arange(270_000 - 5, 270_000, dtype=I32).cuda()
     check_quantised(*svdq.quantize_act_int8_grouped(big, offsets_of([5]), rows=rows), *quantise64(x, None, 1.0))
+
+
+@pytest.mark.parametrize("M,N,K", [(40, 70, 16), (64, 33, 112), (300, 130, 144), (64, 64, 400), (500, 1000, 528), (1024, 2560, 1008), (130, 5120, 1552), (200, 5120, 2064), (40, 48, 640)])
+@pytest.mark.parametrize("at_q,at_w", [(16, 0), (0, 48), (112, 112), (64, 96)])
+def test_operands_that_begin_anywhere_in_a_line(M, N, K, at_q, at_w):
+    """Rows of codes and weights at every sixteenth byte of a memory line."""
+    q, qw = (codes(s, n * K + 256)[at:at + n * K].view(n, K) for s, n, at in ((1, M, at_q), (2, N, at_w)))
+    s, sw, bias = 0.01 + rand(3, M).abs(), 0.01 + rand(4, N).abs(), rand(5, N)
+    for dtype in (BF16, F32):
+        check_product(svdq.linear_w8a8(q, s, qw, sw, bias, out_dtype=dtype), q, s, qw, sw, bias)
+    E = 3
+    qw = codes(6, E * N * K + 256)[at_w:at_w + E * N * K].view(E, N, K)
+    sw, offsets = 0.01 + rand(7, E, N).abs(), offsets_of([M // 3, 0, M - M // 3])
+    check_grouped(svdq.linear_w8a8_grouped(q, s, offsets, qw, sw), q, s, offsets, qw, sw, None)
