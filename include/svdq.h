@@ -387,6 +387,8 @@ int svdq_linear_mxfp4_next(const uint8_t* qx, const uint8_t* sx_e8m0, const void
  *   svdq_linear_w8a8_grouped
  *   svdq_layer_int8_forward  both halves of a layer in one call, of either form.  E == 0: not grouped (rows, offsets and row_rho NULL).
  *                            qx [M, K] and sx [M] receive codes and scales.  y bf16; it may share memory with x, and with nothing else.
+ *                            Both may be NULL where M <= svdq_layer_int8_rows_on_chip (of E, N and K alone) and y and x share none: such a
+ *                            call is one launch, whose codes need not leave the chip (else SVDQ_ERR_INVALID_ARG).
  */
 enum { SVDQ_MAX_K_INT8 = 32768, SVDQ_MAX_EXPERTS = 1024 };
 int svdq_quantize_act_int8(const void* x_bf16, int64_t ldx, const float* inv_lambda, float rho, int gelu,
@@ -406,6 +408,7 @@ typedef struct {
     const float* sw;
     const float* bias;
 } svdq_layer_int8;
+int64_t svdq_layer_int8_rows_on_chip(const svdq_layer_int8* layer);
 int svdq_layer_int8_forward(const svdq_layer_int8* layer, const void* x_bf16, int64_t ldx, int64_t x_rows, const int32_t* rows,
                             const int32_t* offsets, float rho, const float* row_rho, int gelu, int64_t M,
                             int8_t* qx, float* sx, void* y, int64_t ldy, void* stream);

@@ -58,6 +58,7 @@ EXPORTS = {
     "svdq_linear_w8a8": (_i32, [_vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _vp, _i64, _i32, _vp]),
     "svdq_quantize_act_int8_grouped": (_i32, [_vp, _i64, _i64, _vp, _vp, _i32, _vp, _f32, _vp, _i32, _i64, _i32, _vp, _vp, _vp]),
     "svdq_linear_w8a8_grouped": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i64, _i32, _i32, _vp, _i64, _i32, _vp]),
+    "svdq_layer_int8_rows_on_chip": (_i64, [_vp]),
     "svdq_layer_int8_forward": (_i32, [_vp, _vp, _i64, _i64, _vp, _vp, _f32, _vp, _i32, _i64, _vp, _vp, _vp, _i64, _vp]),
     "svdq_debug_group_acc": (_i32, [_vp, _vp, _i64, _i32, _i32, _i64, _i32, _vp, _vp]),
     "svdq_debug_scale_chain": (_i32, [_vp, _f32, _i64, _vp, _vp, _vp]),
@@ -851,6 +852,7 @@ class _W8A8:
                            _tensor("qw", qw, _I8, lead + (N, K), gpu), _tensor("sw", sw, _F32, lead + (N,), gpu),
                            None if bias is None else _tensor("bias", bias, _F32, lead + (N,), gpu))
         layer.address, layer.shape = ctypes.addressof(layer), (layer.E, N, K, gpu)
+        layer.rows_on_chip = (_lib or load_library()).svdq_layer_int8_rows_on_chip(layer.address)
         self._held = (tensors, at, layer)
         return layer
 
@@ -867,12 +869,15 @@ class _W8A8:
         if code != OUT_BF16:
             _refuse("out", out, _BF16, (M, N), gpu)
         if M:
-            # codes and scales of this call alone, from torch's allocator: calls on other streams and captured ones have their own
-            work = torch.empty(M * (K + 4), dtype=torch.uint8, device=x.device)
-            codes = work.data_ptr()
+            codes = scales = None
+            if out is not None or M > layer.rows_on_chip:
+                # of this call alone, from torch's allocator: calls on other streams and captured ones have their own
+                work = torch.empty(M * (K + 4), dtype=torch.uint8, device=x.device)
+                codes = work.data_ptr()
+                scales = codes + M * K
             _check((_lib or load_library()).svdq_layer_int8_forward(
                 layer.address, x.data_ptr(), ldx, x_rows, rows, offsets, rho, row_rho, 1 if gelu else 0, M,
-                codes, codes + M * K, y.data_ptr(), ldy, _raw_stream()), "svdq_layer_int8_forward")
+                codes, scales, y.data_ptr(), ldy, _raw_stream()), "svdq_layer_int8_forward")
         return y
 
 

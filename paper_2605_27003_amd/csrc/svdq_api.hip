@@ -568,9 +568,9 @@ int svdq_layer_forward(const svdq_layer* L, const void* x_bf16, int64_t ldx, flo
     return layer_gemm(L, act, scales, small, fields, expand, r ? hin : nullptr, r ? slices : 1, h, M, staging, y, ldy, stream);
 }
 
-// ---- the 8-bit layer.  Arguments of both forms; offsets null: not grouped.
-static int quantize_int8_check(const svdq::QuantInt8& q) {
-    if (!q.x || !q.qx || !q.sx || q.M < 0) return SVDQ_ERR_INVALID_ARG;
+// ---- the 8-bit layer.  Arguments of both forms; offsets null: not grouped; on_chip: no codes and scales in memory.
+static int quantize_int8_check(const svdq::QuantInt8& q, bool on_chip = false) {
+    if (!q.x || (!on_chip && (!q.qx || !q.sx)) || q.M < 0) return SVDQ_ERR_INVALID_ARG;
     if (!q.row_rho && (!(q.rho > 0.0f) || !(q.rho <= 1.0f))) return SVDQ_ERR_INVALID_ARG;      // also rejects NaN
     if (q.rows && q.x_rows < 0) return SVDQ_ERR_INVALID_ARG;
     if (q.K <= 0 || q.K % 16 || q.K > SVDQ_MAX_K_INT8 || q.ldx < q.K || q.ldx % 8) return SVDQ_ERR_UNSUPPORTED_SHAPE;
@@ -579,15 +579,17 @@ static int quantize_int8_check(const svdq::QuantInt8& q) {
     return q.M > SVDQ_MAX_M ? SVDQ_ERR_UNSUPPORTED_SHAPE : SVDQ_OK;
 }
 
-// plan: the tiles that the product takes
-static int gemm_int8_check(const svdq::GemmInt8& g, int out_dtype, svdq::Int8Plan& plan) {
-    if (!g.qx || !g.sx || !g.qw || !g.sw || !g.y || g.M < 0) return SVDQ_ERR_INVALID_ARG;
+static int gemm_int8_check(const svdq::GemmInt8& g, int out_dtype, bool on_chip = false) {
+    if ((!on_chip && (!g.qx || !g.sx)) || !g.qw || !g.sw || !g.y || g.M < 0) return SVDQ_ERR_INVALID_ARG;
     if (out_dtype != SVDQ_OUT_BF16 && out_dtype != SVDQ_OUT_F32) return SVDQ_ERR_INVALID_ARG;
     if (g.N <= 0 || g.K <= 0 || g.K % 16 || g.K > SVDQ_MAX_K_INT8 || g.ldy < g.N) return SVDQ_ERR_UNSUPPORTED_SHAPE;
     if (!aligned16(g.qx) || !aligned16(g.qw) || !aligned4(g.sx) || !aligned4(g.sw) || !aligned4(g.bias)) return SVDQ_ERR_UNSUPPORTED_SHAPE;
     if ((uintptr_t)g.y & (out_dtype == SVDQ_OUT_F32 ? 3u : 1u)) return SVDQ_ERR_UNSUPPORTED_SHAPE;
-    if (g.M > SVDQ_MAX_M) return SVDQ_ERR_UNSUPPORTED_SHAPE;
-    if (g.M == 0) return SVDQ_OK;
+    return g.M > SVDQ_MAX_M ? SVDQ_ERR_UNSUPPORTED_SHAPE : SVDQ_OK;
+}
+
+// the tiles that a product of checked arguments takes
+static int gemm_int8_plan(const svdq::GemmInt8& g, int out_dtype, svdq::Int8Plan& plan) {
     plan = svdq::int8_plan(g.M, g.N, g.K, g.groups.offsets ? g.groups.E : 0, out_dtype == SVDQ_OUT_F32);
     return plan.cost < 0.0 ? SVDQ_ERR_UNSUPPORTED_SHAPE : SVDQ_OK;
 }
@@ -605,9 +607,10 @@ static int quantize_int8(const svdq::QuantInt8& q, int gelu, void* stream) {
 }
 
 static int linear_int8(const svdq::GemmInt8& g, int out_dtype, void* stream) {
-    svdq::Int8Plan plan{};
-    if (int e = gemm_int8_check(g, out_dtype, plan)) return e;
+    if (int e = gemm_int8_check(g, out_dtype)) return e;
     if (g.M == 0) return SVDQ_OK;
+    svdq::Int8Plan plan{};
+    if (int e = gemm_int8_plan(g, out_dtype, plan)) return e;
     if (int a = check_arch()) return a;
     return hip_status(svdq::launch_gemm_int8(g, plan, out_dtype == SVDQ_OUT_F32, (hipStream_t)stream));
 }
@@ -645,18 +648,35 @@ int svdq_layer_int8_forward(const svdq_layer_int8* L, const void* x_bf16, int64_
     const svdq::Groups groups{offsets, L->E ? L->E : 1};
     const svdq::QuantInt8 q{x_bf16, ldx, rows, x_rows, L->inv_lambda, row_rho, rho, L->K, M, qx, sx, groups};
     const svdq::GemmInt8 g{qx, sx, L->qw, L->sw, L->bias, y, ldy, M, L->N, L->K, groups};
-    if (int e = quantize_int8_check(q)) return e;
-    svdq::Int8Plan plan{};
-    if (int e = gemm_int8_check(g, SVDQ_OUT_BF16, plan)) return e;
+    const bool on_chip = !qx && !sx;
+    if (int e = quantize_int8_check(q, on_chip)) return e;
+    if (int e = gemm_int8_check(g, SVDQ_OUT_BF16, on_chip)) return e;
     if (M == 0) return SVDQ_OK;
-    if (int a = check_arch()) return a;
     // on its own input the output is written behind the quantise launch: in one launch, blocks of other channel tiles still read x
     const int64_t read = rows ? x_rows : M;
     const uintptr_t x0 = (uintptr_t)x_bf16, y0 = (uintptr_t)y;
     const bool meet = read > 0 && x0 < y0 + 2 * ((uintptr_t)(M - 1) * ldy + L->N) && y0 < x0 + 2 * ((uintptr_t)(read - 1) * ldx + L->K);
-    if (!meet && svdq::layer_int8_fits(g)) return hip_status(svdq::launch_layer_int8(q, g, gelu != 0, (hipStream_t)stream));
+    const bool one = !meet && svdq::layer_int8_fits(g);
+    svdq::Int8Plan plan{};
+    if (!one && on_chip) return SVDQ_ERR_INVALID_ARG;
+    if (!one)
+        if (int e = gemm_int8_plan(g, SVDQ_OUT_BF16, plan)) return e;
+    if (int a = check_arch()) return a;
+    if (one) return hip_status(svdq::launch_layer_int8(q, g, gelu != 0, (hipStream_t)stream));
     const hipError_t e = svdq::launch_quantize_int8(q, gelu != 0, (hipStream_t)stream);
     return hip_status(e != hipSuccess ? e : svdq::launch_gemm_int8(g, plan, false, (hipStream_t)stream));
+}
+
+int64_t svdq_layer_int8_rows_on_chip(const svdq_layer_int8* L) {
+    if (!L || L->E < 0 || L->E > SVDQ_MAX_EXPERTS || L->N <= 0 || L->K <= 0 || L->K % 16 || L->K > SVDQ_MAX_K_INT8) return 0;
+    const int32_t grouped = 0;
+    int64_t most = 0, past = (int64_t)1 << 20;                        // more than any layer that fits; fewer rows fit where more do
+    while (past - most > 1) {
+        const int64_t M = (most + past) / 2;
+        const svdq::GemmInt8 g{nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, 0, M, L->N, L->K, {L->E ? &grouped : nullptr, L->E ? L->E : 1}};
+        (svdq::layer_int8_fits(g) ? most : past) = M;
+    }
+    return most;
 }
 
 size_t svdq_gptq_workspace_bytes(int N, int K) {

@@ -2,8 +2,10 @@
 //
 // A block owns 16 tokens by 32 channels, as in the few-token kernel, and makes its tokens' codes itself, for all of K, into LDS (a row a wave, the
 // quantise pass's arithmetic); the first stages of its weights are on their way meanwhile.  The work done again by every channel tile's block (16 K
-// values from L2) costs what the second kernel's start did (replayed from a graph 256 tokens, K = N = 512 take 6.0 us, and 5.7 in two
-// kernels), and the host, which such layers wait for, 8.6 us a call instead of 10.6.  The blocks of the first channel tile also write the codes and scales that the two launches leave.
+// values from L2) costs what the second kernel's start did (replayed from a graph 256 tokens, K = N = 512 take 5.9 us, and 5.7 in two
+// kernels), and the host, which such layers wait for, 6.9 us a call instead of 10.6.  The codes stay on the chip, unless the caller has memory
+// for them: then the blocks of the first channel tile write the codes and scales that the two launches leave (8.3 us a call, since torch's allocator takes
+// 1.4 to find the memory).
 #include "svdq_act.h"
 #include "svdq_int8_dev.h"
 
@@ -51,6 +53,7 @@ void layer_int8_kernel(const QuantInt8 q, const GemmInt8 g) {
 
     // ---- codes of the tile's tokens: rows wave, wave + 4, ...
     {
+        const bool keep = q.qx && at.n0 == 0;
         const int chunks = K >> 3;
         const float* const il = q.inv_lambda ? q.inv_lambda + (at.qw - g.qw) / N : nullptr;           // its expert's: e N K / N
         int at_c[C];
@@ -106,14 +109,14 @@ void layer_int8_kernel(const QuantInt8 q, const GemmInt8 g) {
             float s, inv;
             const bool fine = row_scale(wave_max(top), q.row_rho ? q.row_rho[m0 + r] : q.rho, s, inv);
             if (lane == 0) *reinterpret_cast<__attribute__((address_space(3))) float*>((lds_byte*)(uintptr_t)(lds0 + OFF_SCALES + r * 4)) = s;
-            if (lane == 0 && at.n0 == 0) q.sx[m0 + r] = s;
+            if (lane == 0 && keep) q.sx[m0 + r] = s;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 const uint2 o = codes8(xs[c], inv, fine);
                 if (!in[c]) continue;
                 const int k8 = at_c[c], stage = k8 >> 4, piece = (k8 >> 1) & 7;          // eight k each: stages of sixteen, pieces of two
                 lds_write8_pinned(lds0 + (stage * TOK + r) * BK + ((piece ^ ((r >> 1) & 7)) << 4) + (k8 & 1) * 8, o);
-                if (at.n0 == 0) reinterpret_cast<uint2*>(q.qx + (int64_t)(m0 + r) * K)[k8] = o;
+                if (keep) reinterpret_cast<uint2*>(q.qx + (int64_t)(m0 + r) * K)[k8] = o;
             }
         }
     }
@@ -189,8 +192,8 @@ void launch(const QuantInt8& q, const GemmInt8& g, const bool gelu, const int bl
 
 }  // namespace
 
-// Up to two blocks for every CU, with a K that lets two of them have one's LDS (16 tokens, N = 5120, K = 1024: 8.6 us, 10.5 in two launches); a longer
-// one with a row for each wave (one token, K = N = 4096: 8.5 and 10.1; but 16 tokens 13.8 and 10.1).
+// Up to two blocks for every CU, with a K that lets two of them have one's LDS (16 tokens, N = 5120, K = 1024: 7.5 us, 10.5 in two launches); a longer
+// one with a row for each wave (one token, K = N = 4096: 7.1 and 10.1; but 16 tokens 13.8 and 10.1).
 bool layer_int8_fits(const GemmInt8& g) {
     const int64_t mt = g.groups.offsets ? g.M / TOK + (g.M < g.groups.E ? g.M : g.groups.E) : (g.M + TOK - 1) / TOK;
     return (g.K <= 1408 || (g.K <= 4096 && g.M <= NW)) && mt * (((int64_t)g.N + BN - 1) / BN) <= 512;

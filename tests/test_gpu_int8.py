@@ -434,3 +434,22 @@ def test_operands_that_begin_anywhere_in_a_line(M, N, K, at_q, at_w):
     qw = codes(6, E * N * K + 256)[at_w:at_w + E * N * K].view(E, N, K)
     sw, offsets = 0.01 + rand(7, E, N).abs(), offsets_of([M // 3, 0, M - M // 3])
     check_grouped(svdq.linear_w8a8_grouped(q, s, offsets, qw, sw), q, s, offsets, qw, sw, None)
+
+
+@pytest.mark.parametrize("N,K,E", [(512, 512, 0), (2048, 1408, 0), (640, 4096, 0), (512, 528, 8), (256, 64, 300)])
+def test_last_rows_whose_codes_stay_on_the_chip(N, K, E):
+    """The most rows that are one launch without memory for codes, and one more."""
+    lead = (E,) if E else ()
+    qw, sw, bias, il = codes(1, *lead, N, K), 0.001 * rand(2, *lead, N).abs(), rand(3, *lead, N), 0.5 + rand(4, *lead, K).abs()
+    module = svdq.W8A8Experts(il, qw, sw, bias) if E else svdq.W8A8Linear(il, qw, sw, bias)
+    most = module._descriptor().rows_on_chip
+    for M in (most, most + 1):
+        x = rand(5, M, K).to(BF16)
+        if E:
+            offsets = offsets_of([1] * min(E, M) + [0] * (E - min(E, M)))
+            offsets[-1] = M                                            # the last expert has the rest: as many tiles as there can be
+            qx, sx = svdq.quantize_act_int8_grouped(x, offsets, il, 0.9)
+            want, got = svdq.linear_w8a8_grouped(qx, sx, offsets, qw, sw, bias), module.forward(x, offsets, 0.9)
+        else:
+            want, got = svdq.linear_w8a8(*svdq.quantize_act_int8(x, il, 0.9), qw, sw, bias), module.forward(x, 0.9)
+        assert torch.equal(got, want)

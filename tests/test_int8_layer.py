@@ -107,3 +107,24 @@ def test_descriptor_follows_memory_given_to_the_same_tensor():
     layer.qw.data = torch.zeros((32, 64), dtype=torch.int8)
     with pytest.raises(ValueError, match="inv_lambda"):
         layer._descriptor()
+
+
+def test_rows_whose_codes_stay_on_the_chip():
+    """Without memory for codes and scales: up to svdq_layer_int8_rows_on_chip rows, and where y is not x."""
+    lib = binding.load_library()
+
+    def rows(E, N, K):
+        layer = binding._LayerInt8(E, N, K, A, A, A, A)
+        return lib.svdq_layer_int8_rows_on_chip(ctypes.addressof(layer))
+    # 512 tiles of 16 x 32 up to K = 1408; four rows of a longer K; nothing beyond 4096
+    assert [rows(*a) for a in ((0, 512, 512), (0, 512, 1408), (0, 512, 1424), (0, 32, 4096), (0, 32, 4112), (0, 16384, 64), (0, 16416, 64))] == [512, 512, 4, 4, 0, 16, 0]
+    # an expert with rows can add a tile that is not full
+    assert rows(8, 512, 512) == 16 * (32 - 8) + 15 and rows(1024, 512, 512) == 31 and rows(1, 32, 64) == 16 * 511 + 15
+    assert [rows(*a) for a in ((0, 0, 64), (0, 32, 72), (-1, 32, 64), (1025, 32, 64), (0, 32, 0))] == [0] * 5 and lib.svdq_layer_int8_rows_on_chip(None) == 0
+    far = 1 << 30
+    layer = binding._LayerInt8(0, 512, 512, A, A, A, A)
+    ok = dict(L=ctypes.addressof(layer), x=A, ldx=512, x_rows=0, rows=Z, offsets=Z, rho=0.9, row_rho=Z, gelu=0, M=4, qx=Z, sx=Z, y=far, ldy=512)
+    call = lambda **kw: lib.svdq_layer_int8_forward(*{**ok, **kw}.values(), Z)
+    assert call(M=0) == 0
+    for kw in (dict(M=513), dict(y=A), dict(qx=A), dict(sx=A)):
+        assert call(**kw) == INV, kw
