@@ -387,7 +387,7 @@ int svdq_linear_mxfp4_next(const uint8_t* qx, const uint8_t* sx_e8m0, const void
  *   svdq_linear_w8a8_grouped
  *   svdq_layer_int8_forward  both halves of a layer in one call, of either form.  E == 0: not grouped (rows, offsets and row_rho NULL).
  *                            qx [M, K] and sx [M] receive codes and scales.  y bf16; it may share memory with x, and with nothing else.
- *                            Both may be NULL where M <= svdq_layer_int8_rows_on_chip (of E, N and K alone) and y and x share none: such a
+ *                            qx and sx may both be NULL where M <= svdq_layer_int8_rows_on_chip (of E, N and K alone) and y and x share none: such a
  *                            call is one launch, whose codes need not leave the chip (else SVDQ_ERR_INVALID_ARG).
  */
 enum { SVDQ_MAX_K_INT8 = 32768, SVDQ_MAX_EXPERTS = 1024 };
