@@ -95,9 +95,10 @@ def _ptr(t):
 # hipStream_t of the current stream of the current device.  torch.cuda.current_stream() builds a Stream object for it:
 # 2.8 us against 0.1 us, of the 12 us that the host needs for a layer with few tokens.  Where torch has renamed its own
 # functions, the public way.
-def _raw_stream():
+def _raw_stream(current=None):
+    """current: the current device, where the caller knows it."""
     try:
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice() if current is None else current)
     except AttributeError:
         return torch.cuda.current_stream().cuda_stream
 
@@ -751,7 +752,7 @@ def quantize_act_int8(x_bf16, inv_lambda=None, rho=1.0, gelu=False, out=None):
     qx, sx = _quantize_int8_out(out, M, K, x_bf16, gpu)
     if M:                            # an empty tensor has no address
         _check((_lib or load_library()).svdq_quantize_act_int8(x_bf16.data_ptr(), ldx, il, float(rho), 1 if gelu else 0, M, K, qx.data_ptr(), sx.data_ptr(),
-                                                               _raw_stream()), "svdq_quantize_act_int8")
+                                                               _raw_stream(gpu)), "svdq_quantize_act_int8")
     return qx, sx
 
 
@@ -777,7 +778,7 @@ def linear_w8a8(qx, sx, qw, sw, bias=None, out=None, out_dtype=torch.bfloat16):
     pb = None if bias is None else _vector("bias", bias, _F32, N, gpu)
     y, ldy, code = _linear_out(out, M, N, out_dtype, qx, gpu)
     if M:
-        _check((_lib or load_library()).svdq_linear_w8a8(pq, ps, pw, pc, pb, M, N, K, y.data_ptr(), ldy, code, _raw_stream()), "svdq_linear_w8a8")
+        _check((_lib or load_library()).svdq_linear_w8a8(pq, ps, pw, pc, pb, M, N, K, y.data_ptr(), ldy, code, _raw_stream(gpu)), "svdq_linear_w8a8")
     return y
 
 
@@ -801,7 +802,7 @@ def quantize_act_int8_grouped(x_bf16, offsets, inv_lambda=None, rho=1.0, rows=No
     qx, sx = _quantize_int8_out(out, M, K, x_bf16, gpu)
     if M:
         _check((_lib or load_library()).svdq_quantize_act_int8_grouped(
-            x_bf16.data_ptr(), ldx, x_rows, r, o, E, il, ratio, row_rho, 1 if gelu else 0, M, K, qx.data_ptr(), sx.data_ptr(), _raw_stream()),
+            x_bf16.data_ptr(), ldx, x_rows, r, o, E, il, ratio, row_rho, 1 if gelu else 0, M, K, qx.data_ptr(), sx.data_ptr(), _raw_stream(gpu)),
             "svdq_quantize_act_int8_grouped")
     return qx, sx
 
@@ -818,7 +819,7 @@ def linear_w8a8_grouped(qx, sx, offsets, qw, sw, bias=None, out=None, out_dtype=
     o = _vector("offsets", offsets, _I32, E + 1, gpu)
     y, ldy, code = _linear_out(out, M, N, out_dtype, qx, gpu)
     if M:
-        _check((_lib or load_library()).svdq_linear_w8a8_grouped(pq, ps, pw, pc, pb, o, E, M, N, K, y.data_ptr(), ldy, code, _raw_stream()), "svdq_linear_w8a8_grouped")
+        _check((_lib or load_library()).svdq_linear_w8a8_grouped(pq, ps, pw, pc, pb, o, E, M, N, K, y.data_ptr(), ldy, code, _raw_stream(gpu)), "svdq_linear_w8a8_grouped")
     return y
 
 
@@ -836,24 +837,29 @@ class _W8A8:
         self._descriptor()
 
     def _descriptor(self):
-        """svdq_layer_int8 of the tensors that the layer holds now, checked when they, or the memory that they have, have changed.
-        The caller keeps it through its call."""
+        """svdq_layer_int8 of the tensors that the layer holds now, checked when they, or what a kernel goes by of them (memory, type, shape,
+        order), have changed.  The caller keeps it through its call."""
         inv_lambda, qw, sw, bias = tensors = self.inv_lambda, self.qw, self.sw, self.bias
-        at = (None if inv_lambda is None else inv_lambda.data_ptr(), qw.data_ptr(), sw.data_ptr(), None if bias is None else bias.data_ptr())
         held = self._held
         if held is not None:
-            (a, b, c, d), was, layer = held
-            if a is inv_lambda and b is qw and c is sw and d is bias and at == was:
+            (a, b, c, d), (at, weights, channels, inputs), layer = held
+            # (attributes only, 0.7 us of a call: making and comparing views costs more)
+            if (a is inv_lambda and b is qw and c is sw and d is bias
+                    and at == (None if a is None else a.data_ptr(), b.data_ptr(), c.data_ptr(), None if d is None else d.data_ptr())
+                    and b.dtype is _I8 and c.dtype is _F32 and b.shape == weights and c.shape == channels and b.is_contiguous() and c.is_contiguous()
+                    and (a is None or (a.dtype is _F32 and a.shape == inputs and a.is_contiguous()))
+                    and (d is None or (d.dtype is _F32 and d.shape == channels and d.is_contiguous()))):
                 return layer
         if qw.dim() != 2 + self.GROUPED:
             raise ValueError(f"qw: {'[E, N, K]' if self.GROUPED else '[N, K]'} is needed, not {tuple(qw.shape)}")
         lead, (N, K), gpu = tuple(qw.shape[:-2]), qw.shape[-2:], qw.get_device()
-        layer = _LayerInt8(lead[0] if lead else 0, N, K, None if inv_lambda is None else _tensor("inv_lambda", inv_lambda, _F32, lead + (K,), gpu),
-                           _tensor("qw", qw, _I8, lead + (N, K), gpu), _tensor("sw", sw, _F32, lead + (N,), gpu),
-                           None if bias is None else _tensor("bias", bias, _F32, lead + (N,), gpu))
+        weights, channels, inputs = lead + (N, K), lead + (N,), lead + (K,)
+        at = (None if inv_lambda is None else _tensor("inv_lambda", inv_lambda, _F32, inputs, gpu), _tensor("qw", qw, _I8, weights, gpu),
+              _tensor("sw", sw, _F32, channels, gpu), None if bias is None else _tensor("bias", bias, _F32, channels, gpu))
+        layer = _LayerInt8(lead[0] if lead else 0, N, K, *at)
         layer.address, layer.shape = ctypes.addressof(layer), (layer.E, N, K, gpu)
         layer.rows_on_chip = (_lib or load_library()).svdq_layer_int8_rows_on_chip(layer.address)
-        self._held = (tensors, at, layer)
+        self._held = (tensors, (at, weights, channels, inputs), layer)
         return layer
 
     def __getstate__(self):
@@ -861,23 +867,31 @@ class _W8A8:
         return {**self.__dict__, "_held": None}
 
     def _forward(self, x, layer, gpu, rows, offsets, rho, row_rho, gelu, M, out):
+        """M: None for the rows of x."""
         _, N, K, home = layer.shape
         x_rows, _, ldx = _matrix("x", x, (_BF16,), gpu, K)
         if home != gpu:
             raise ValueError(f"x is on GPU {gpu}, the layer on {self.qw.device}")
-        y, ldy, code = _linear_out(out, M, N, _BF16, x, gpu)
-        if code != OUT_BF16:
-            _refuse("out", out, _BF16, (M, N), gpu)
+        if M is None:
+            M = x_rows
+        if out is None:
+            y, ldy = x.new_empty(M, N), N
+        else:
+            y, ldy, code = _linear_out(out, M, N, _BF16, x, gpu)
+            if code != OUT_BF16:
+                _refuse("out", out, _BF16, (M, N), gpu)
         if M:
             codes = scales = None
             if out is not None or M > layer.rows_on_chip:
                 # of this call alone, from torch's allocator: calls on other streams and captured ones have their own
-                work = torch.empty(M * (K + 4), dtype=torch.uint8, device=x.device)
+                work = x.new_empty(M * (K // 2 + 2))
                 codes = work.data_ptr()
                 scales = codes + M * K
-            _check((_lib or load_library()).svdq_layer_int8_forward(
+            rc = (_lib or load_library()).svdq_layer_int8_forward(
                 layer.address, x.data_ptr(), ldx, x_rows, rows, offsets, rho, row_rho, 1 if gelu else 0, M,
-                codes, scales, y.data_ptr(), ldy, _raw_stream()), "svdq_layer_int8_forward")
+                codes, scales, y.data_ptr(), ldy, _raw_stream(gpu))
+            if rc:
+                _check(rc, "svdq_layer_int8_forward")
         return y
 
 
@@ -888,7 +902,7 @@ class W8A8Linear(_W8A8):
 
     def forward(self, x_bf16, rho=1.0, gelu=False, out=None):
         """x [M,K] bf16 -> y [M,N] bf16: quantize_act_int8 and linear_w8a8 in one call.  out may share memory with x."""
-        return self._forward(x_bf16, self._descriptor(), _gpu(x_bf16), None, None, float(rho), None, gelu, x_bf16.shape[0], out)
+        return self._forward(x_bf16, self._descriptor(), _gpu(x_bf16), None, None, float(rho), None, gelu, None, out)
 
 
 class W8A8Experts(_W8A8):

@@ -128,3 +128,39 @@ def test_rows_whose_codes_stay_on_the_chip():
     assert call(M=0) == 0
     for kw in (dict(M=513), dict(y=A), dict(qx=A), dict(sx=A)):
         assert call(**kw) == INV, kw
+
+
+@pytest.mark.parametrize("grouped", [False, True])
+def test_descriptor_follows_views_given_to_the_same_tensor(grouped):
+    """A smaller view, another type or another order of the memory that a held tensor has already: taken up, or refused."""
+    E, N, K = 2, 48, 48
+    lead = (E,) if grouped else ()
+
+    def made():
+        return (svdq.W8A8Experts if grouped else svdq.W8A8Linear)(torch.ones(lead + (K,)), torch.zeros(lead + (N, K), dtype=torch.int8), torch.ones(lead + (N,)),
+                                                                  torch.ones(lead + (N,)))
+    layer = made()
+    first = layer._descriptor()
+    for name in ("qw", "sw", "bias"):                                 # fewer channels, from where the held ones begin
+        held = getattr(layer, name)
+        held.data = held.data.flatten()[:held.numel() // 3].view(*lead, N // 3, *held.shape[1 + grouped:])
+    now = layer._descriptor()
+    assert (now.N, now.K, now.qw, now.sw, now.bias) == (N // 3, K, first.qw, first.sw, first.bias) and now.shape[1] == N // 3
+    # one tensor alone no longer fits the others, is of another type, or has its values in another order
+    for name in ("inv_lambda", "qw", "sw", "bias"):
+        half = lambda t: t.flatten()[:t.numel() // 2].view(*t.shape[:-1], t.shape[-1] // 2)
+        for change in (half, lambda t: t.view(torch.uint8 if t.dtype is torch.int8 else torch.int32), lambda t: t[..., None],
+                       lambda t: t.as_strided(t.shape, (0,) * t.dim()), lambda t: t.mT if t.shape == lead + (N, K) and t.dtype is torch.int8 else t[..., :1]):
+            layer = made()
+            held = getattr(layer, name)
+            layer._descriptor()
+            held.data = change(held.data)
+            with pytest.raises(ValueError):
+                layer._descriptor()
+            with pytest.raises(ValueError):                           # not on the second call either
+                layer._descriptor()
+    layer = made()
+    layer._descriptor()
+    layer.qw.transpose_(-1, -2)
+    with pytest.raises(ValueError, match="qw"):
+        layer._descriptor()
