@@ -381,7 +381,7 @@ int svdq_linear_mxfp4_next(const uint8_t* qx, const uint8_t* sx_e8m0, const void
  * Offsets that break this are read as their running maximum, cut to [0, M]: rows may then be another expert's, but no access
  * leaves the arrays.
  *   svdq_quantize_act_int8_grouped   row i is made of row rows[i] of x [x_rows, ldx] (rows: M int32 on the device, in any order and any number of
- *                            times each; a number outside [0, x_rows) counts as a row of zeros), or with rows NULL of row i
+ *                            times each; a number outside [0, x_rows) counts as a row of zeros; with x_rows 0 x may be NULL), or with rows NULL of row i
  *                            of x [M, ldx]; row_rho [M] binary32 on the device holds each row's ratio (not checked: one that is not
  *                            positive gives scale 0, a NaN scale NaN), or NULL for rho
  *   svdq_linear_w8a8_grouped

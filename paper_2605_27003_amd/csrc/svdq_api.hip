@@ -570,7 +570,8 @@ int svdq_layer_forward(const svdq_layer* L, const void* x_bf16, int64_t ldx, flo
 
 // ---- the 8-bit layer.  Arguments of both forms; offsets null: not grouped; on_chip: no codes and scales in memory.
 static int quantize_int8_check(const svdq::QuantInt8& q, bool on_chip = false) {
-    if (!q.x || (!on_chip && (!q.qx || !q.sx)) || q.M < 0) return SVDQ_ERR_INVALID_ARG;
+    const bool no_x = q.rows && q.x_rows == 0;                        // every row number is outside: nothing is read
+    if ((!q.x && !no_x) || (!on_chip && (!q.qx || !q.sx)) || q.M < 0) return SVDQ_ERR_INVALID_ARG;
     if (!q.row_rho && (!(q.rho > 0.0f) || !(q.rho <= 1.0f))) return SVDQ_ERR_INVALID_ARG;      // also rejects NaN
     if (q.rows && q.x_rows < 0) return SVDQ_ERR_INVALID_ARG;
     if (q.K <= 0 || q.K % 16 || q.K > SVDQ_MAX_K_INT8 || q.ldx < q.K || q.ldx % 8) return SVDQ_ERR_UNSUPPORTED_SHAPE;

@@ -453,3 +453,14 @@ def test_last_rows_whose_codes_stay_on_the_chip(N, K, E):
         else:
             want, got = svdq.linear_w8a8(*svdq.quantize_act_int8(x, il, 0.9), qw, sw, bias), module.forward(x, 0.9)
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 40, 272), (700, 600, 1552)])
+def test_rows_of_an_x_without_rows(M, N, K):
+    """Zeros all of them, in one launch and in two: codes and scales 0, outputs the biases."""
+    E = 2
+    x, rows, offsets = torch.empty((0, K), dtype=BF16, device="cuda"), torch.arange(-1, M - 1, dtype=I32).cuda(), offsets_of([M // 3, M - M // 3])
+    il, qw, sw, bias = 0.5 + rand(1, E, K).abs(), codes(2, E, N, K), rand(3, E, N).abs(), rand(4, E, N)
+    qx, sx = svdq.quantize_act_int8_grouped(x, offsets, il, 0.9, rows=rows)
+    assert not qx.any() and not sx.any()
+    assert torch.equal(svdq.W8A8Experts(il, qw, sw, bias).forward(x, offsets, 0.9, rows=rows), bias[experts_of(offsets, M)].to(BF16))

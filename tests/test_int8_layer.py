@@ -164,3 +164,15 @@ def test_descriptor_follows_views_given_to_the_same_tensor(grouped):
     layer.qw.transpose_(-1, -2)
     with pytest.raises(ValueError, match="qw"):
         layer._descriptor()
+
+
+def test_rows_of_an_x_without_rows_are_not_refused():
+    """An empty tensor has no address: x is needed only where a row number can lie within it.  (K = 520 and ldy = 96 are refused behind that check.)"""
+    lib = binding.load_library()
+    ok = dict(x=Z, ldx=520, x_rows=0, rows=A, offsets=A, E=3, il=A, rho=0.9, row_rho=Z, gelu=0, M=4, K=520, qx=A, sx=A)
+    call = lambda **kw: lib.svdq_quantize_act_int8_grouped(*{**ok, **kw}.values(), Z)
+    assert call() == SHAPE and call(x_rows=1) == INV and call(rows=Z) == INV and call(qx=Z) == INV
+    layer = binding._LayerInt8(2, 100, 512, A, A, A, A)
+    ok = dict(layer=ctypes.addressof(layer), x=Z, ldx=512, x_rows=0, rows=A, offsets=A, rho=0.9, row_rho=Z, gelu=0, M=4, qx=A, sx=A, y=A, ldy=96)
+    call = lambda **kw: lib.svdq_layer_int8_forward(*{**ok, **kw}.values(), Z)
+    assert call() == SHAPE and call(x_rows=1) == INV and call(rows=Z) == INV
