@@ -364,7 +364,7 @@ int svdq_linear_mxfp4_next(const uint8_t* qx, const uint8_t* sx_e8m0, const void
  *   y[m,n] = (sum_k q[m,k] qw[n,k]) * s[m] * sw[n] + bias[n]
  * each step of the codes and scales a single IEEE binary32 operation (bit-exact), the sum exact in 32-bit integers, y rounded once
  * from binary32.  A row of x with a NaN or an infinity (or whose x^ overflows) gets scale NaN and codes 0, so its row of y is NaN
- * and no other is; a scale that would not be a normal number is 0, with codes 0.  No low-rank branch.
+ * and no other is; a scale that would not be a normal number (0, subnormal, infinite) is 0, with codes 0.  No low-rank branch.
  * Codes and weights are row-major, one byte a value, as such checkpoints hold them; nothing is packed.
  *
  *   svdq_quantize_act_int8   x_bf16 [M, ldx] bf16, ldx >= K, ldx % 8 == 0; inv_lambda [K] binary32 or NULL (ones); rho in (0, 1];

@@ -10,11 +10,12 @@ constexpr int BK = 128;          // k (and bytes) of a row per stage of a produc
 constexpr float QMAX8 = 127.0f;  // codes are symmetric: -128 is not used
 
 // A row's scale from the bit pattern of its largest magnitude (a NaN's or an infinity's is past every finite one's), and what its values are
-// multiplied with; false: codes 0, the scale NaN where the row or its ratio is none, 0 where it would not be a normal number.
+// multiplied with; false: codes 0, the scale NaN where the row or its ratio is none, 0 where it would not be a normal number (an infinite one comes of a
+// row's own ratio, which nobody checks).
 __device__ __forceinline__ bool row_scale(const uint32_t top, const float rho, float& s, float& inv) {
     const bool finite = top < 0x7f800000u;
     s = __fdiv_rn(__fmul_rn(rho, bits_f(top)), QMAX8);
-    const bool fine = finite && s >= 1.17549435e-38f;
+    const bool fine = finite && s >= 1.17549435e-38f && s <= 3.40282347e38f;
     inv = fine ? __fdiv_rn(1.0f, s) : 0.0f;
     if (!fine) s = finite && s == s ? 0.0f : bits_f(0x7fc00000u);
     return fine;

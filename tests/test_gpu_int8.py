@@ -464,3 +464,20 @@ def test_rows_of_an_x_without_rows(M, N, K):
     qx, sx = svdq.quantize_act_int8_grouped(x, offsets, il, 0.9, rows=rows)
     assert not qx.any() and not sx.any()
     assert torch.equal(svdq.W8A8Experts(il, qw, sw, bias).forward(x, offsets, 0.9, rows=rows), bias[experts_of(offsets, M)].to(BF16))
+
+
+@pytest.mark.parametrize("K,N", [(272, 40), (2064, 600)])
+def test_scales_that_would_be_infinite(K, N):
+    """From a row's own ratio: 0, as every scale that is no normal number, with codes 0 and the biases as outputs; the largest finite scale is an ordinary one."""
+    M = 6
+    x = torch.zeros((M, K), dtype=BF16, device="cuda")
+    x[:, 1], x[:, 2] = 2.0, -1.0
+    rho = torch.tensor([1.0, float("inf"), 3e38, 1.5e38, 1.7e38, -float("inf")]).cuda()   # 2 rho past 3.4e38: rows 1, 2; and -inf, not positive
+    offsets, qw, sw, bias = offsets_of([2, 4]), codes(1, 2, N, K), rand(2, 2, N).abs() * 1e-38, rand(3, 2, N)
+    none = torch.tensor([False, True, True, False, False, True], device="cuda")
+    qx, sx = svdq.quantize_act_int8_grouped(x, offsets, rho=rho)
+    assert bool((sx[none] == 0).all()) and not qx[none].any()
+    check_quantised(qx[~none], sx[~none], *quantise64(x[~none], None, rho[~none]))
+    y = svdq.W8A8Experts(None, qw, sw, bias).forward(x, offsets, rho)
+    assert torch.equal(y[none], bias[experts_of(offsets, M)].to(BF16)[none]) and bool(torch.isfinite(y[0]).all())
+    assert torch.equal(y.view(torch.int16), svdq.linear_w8a8_grouped(qx, sx, offsets, qw, sw, bias).view(torch.int16))
