@@ -40,8 +40,9 @@ struct GemmInt8 {
     Groups groups;
 };
 struct Int8Plan;
+struct Int8Kernel;
 hipError_t launch_gemm_int8(const GemmInt8& g, const Int8Plan& p, bool out_f32, hipStream_t stream);
-hipError_t launch_gemm_int8_few(const GemmInt8& g, const Int8Plan& p, bool out_f32, hipStream_t stream);     // the few-token kernel's tiles
+hipError_t launch_gemm_int8_few(const GemmInt8& g, const Int8Kernel& k, bool out_f32, hipStream_t stream);     // the few-token kernel's tiles
 
 // Both halves in one launch, for layers that fit it (bf16 outputs).  x and y share no memory.
 bool layer_int8_fits(const GemmInt8& g);

@@ -2,6 +2,7 @@
 #pragma once
 #include "svdq.h"
 #include "svdq_int8.h"
+#include "svdq_int8_plan.h"
 #include "svdq_lds.h"
 
 namespace svdq {
@@ -163,12 +164,9 @@ struct GroupTiles {
 template <bool GROUPED, int BM, int BN> struct TilesOf { using type = DenseTiles<BM, BN>; };
 template <int BM, int BN> struct TilesOf<true, BM, BN> { using type = GroupTiles<BM, BN>; };
 
-// Every expert with rows adds at most one row tile that is not full.
-inline int64_t tiles_there_can_be(const GemmInt8& g, const int bm, const int bn) {
-    const int64_t mt = g.groups.offsets ? g.M / bm + (g.M < g.groups.E ? g.M : g.groups.E) : (g.M + bm - 1) / bm;
-    return mt * (((int64_t)g.N + bn - 1) / bn);
+// As many blocks as there can be tiles, in whole rounds of the numbering.
+inline int most_tiles(const GemmInt8& g, const int bm, const int bn) {
+    return (int)((int8_tiles(g.M, g.N, g.groups.offsets ? g.groups.E : 0, bm, bn) + 255) / 256 * 256);
 }
-// As many blocks.
-inline int most_tiles(const GemmInt8& g, const int bm, const int bn) { return (int)((tiles_there_can_be(g, bm, bn) + 255) / 256 * 256); }
 
 }  // namespace svdq

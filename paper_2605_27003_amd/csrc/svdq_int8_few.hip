@@ -181,11 +181,11 @@ hipError_t launch(const GemmInt8& g, const bool out_f32, hipStream_t stream) {
 
 // Thirty-two channels a block halve the tokens' transfers (24 tokens, 5120 x 5120: 7.8 against 9.2 us); sixteen, on eight waves, where there
 // are few blocks (one token, N = 1024, K = 13824: 5.6 against 7.4 us).
-hipError_t launch_gemm_int8_few(const GemmInt8& g, const Int8Plan& p, bool out_f32, hipStream_t stream) {
-    switch (p.tiles) {
+hipError_t launch_gemm_int8_few(const GemmInt8& g, const Int8Kernel& k, bool out_f32, hipStream_t stream) {
+    switch (k.tiles) {
         case Int8Tiles::FEW_16x16: return launch<16, 16, 8, 2>(g, out_f32, stream);
-        case Int8Tiles::FEW_16x32:                                    // one round of blocks: a stage more in flight (6.9 against 7.8 us at N = K = 5120)
-            if (!g.groups.offsets && g.M <= 16 && g.N <= 32 * CUS) return launch<16, 32, 4, 3>(g, out_f32, stream);
+        case Int8Tiles::FEW_16x32:
+            if (k.depth == 3) return launch<16, 32, 4, 3>(g, out_f32, stream);
             return launch<16, 32, 4, 2>(g, out_f32, stream);
         case Int8Tiles::FEW_32x16: return launch<32, 16, 8, 2>(g, out_f32, stream);
         default: return launch<32, 32, 4, 2>(g, out_f32, stream);

@@ -195,8 +195,7 @@ void launch(const QuantInt8& q, const GemmInt8& g, const bool gelu, const int bl
 // Up to two blocks for every CU, with a K that lets two of them have one's LDS (16 tokens, N = 5120, K = 1024: 7.5 us, 10.5 in two launches); a longer
 // one with a row for each wave (one token, K = N = 4096: 7.1 and 10.1; but 16 tokens 13.8 and 10.1).
 bool layer_int8_fits(const GemmInt8& g) {
-    const int64_t mt = g.groups.offsets ? g.M / TOK + (g.M < g.groups.E ? g.M : g.groups.E) : (g.M + TOK - 1) / TOK;
-    return (g.K <= 1408 || (g.K <= 4096 && g.M <= NW)) && mt * (((int64_t)g.N + BN - 1) / BN) <= 512;
+    return (g.K <= 1408 || (g.K <= 4096 && g.M <= NW)) && int8_tiles(g.M, g.N, g.groups.offsets ? g.groups.E : 0, TOK, BN) <= 512;
 }
 
 hipError_t launch_layer_int8(const QuantInt8& q, const GemmInt8& g, const bool gelu, hipStream_t stream) {

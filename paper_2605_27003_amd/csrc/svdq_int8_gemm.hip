@@ -343,25 +343,21 @@ hipError_t launch_tiles(const GemmInt8& g, const bool out_f32, hipStream_t strea
 }  // namespace
 
 hipError_t launch_gemm_int8(const GemmInt8& g, const Int8Plan& p, bool out_f32, hipStream_t stream) {
-    const Int8TileShape shape = int8_tile_shape(p.tiles);
-    const int64_t tiles = tiles_there_can_be(g, shape.bm, shape.bn);
-    // rows fetched by whole lines, a block alone on its CU: where enough blocks share what L2 gives.  (Few wait for latency, and have less under way so:
-    // one tile of 128 x 128 takes up to 1.29 times as long, 48 to 256 tiles 0.7 to 1.1 times, 0.94 in the mean of 80 products.)
-    const bool lines = g.K % BK && tiles > 48 && tiles <= 256;
+    const Int8Kernel k = int8_kernel(p.tiles, g.M, g.N, g.K, g.groups.offsets ? g.groups.E : 0);
     switch (p.tiles) {
         case Int8Tiles::T64x32: return launch_tiles<Int8Tile<64, 32, 2, 2, 4>>(g, out_f32, stream);
         case Int8Tiles::T64x64: return launch_tiles<Int8Tile<64, 64, 2, 2, 4>>(g, out_f32, stream);
         case Int8Tiles::T64x128:
-            if (lines) return launch_tiles<Int8Tile<64, 128, 2, 4, 4, true>>(g, out_f32, stream);
+            if (k.lines) return launch_tiles<Int8Tile<64, 128, 2, 4, 4, true>>(g, out_f32, stream);
             return launch_tiles<Int8Tile<64, 128, 2, 4, 3>>(g, out_f32, stream);
-        case Int8Tiles::T128x128:                                     // a block alone on its CU, or two
-            if (lines) return launch_tiles<Int8Tile<128, 128, 2, 4, 4, true>>(g, out_f32, stream);
-            if (tiles <= 256) return launch_tiles<Int8Tile<128, 128, 2, 4, 4>>(g, out_f32, stream);
+        case Int8Tiles::T128x128:
+            if (k.lines) return launch_tiles<Int8Tile<128, 128, 2, 4, 4, true>>(g, out_f32, stream);
+            if (k.depth == 4) return launch_tiles<Int8Tile<128, 128, 2, 4, 4>>(g, out_f32, stream);
             return launch_tiles<Int8Tile<128, 128, 2, 4, 2>>(g, out_f32, stream);
         case Int8Tiles::T256x128: return launch_tiles<Int8Tile<256, 128, 4, 2, 2>>(g, out_f32, stream);
         case Int8Tiles::T256x160: return launch_tiles<Int8Tile<256, 160, 4, 2, 2>>(g, out_f32, stream);
         case Int8Tiles::T256x256: return launch_tiles<Int8Tile<256, 256, 2, 4, 2>>(g, out_f32, stream);
-        default: return launch_gemm_int8_few(g, p, out_f32, stream);
+        default: return launch_gemm_int8_few(g, k, out_f32, stream);
     }
 }
 

@@ -85,4 +85,33 @@ inline Int8Plan int8_plan(int64_t rows, int N, int K, int experts, bool out_f32)
     return best;
 }
 
+// Row tiles by channel tiles that there can be: every expert with rows adds at most one row tile that is not full.
+inline int64_t int8_tiles(int64_t rows, int N, int experts, int bm, int bn) {
+    const int64_t mt = experts ? rows / bm + (rows < experts ? rows : experts) : (rows + bm - 1) / bm;
+    return mt * (((int64_t)N + bn - 1) / bn);
+}
+
+// The kernel for tiles: how many stages ahead it requests, and whether it fetches rows by whole memory lines.
+struct Int8Kernel {
+    Int8Tiles tiles;
+    int depth;
+    bool lines;
+};
+inline Int8Kernel int8_kernel(Int8Tiles t, int64_t rows, int N, int K, int experts) {
+    const Int8TileShape s = int8_tile_shape(t);
+    const int64_t tiles = int8_tiles(rows, N, experts, s.bm, s.bn);
+    // rows fetched by whole lines, a block alone on its CU: where enough blocks share what L2 gives.  (Few wait for latency, and have less under way so:
+    // one tile of 128 x 128 takes up to 1.29 times as long, 48 to 256 tiles 0.7 to 1.1 times, 0.94 in the mean of 80 products.)
+    const bool lines = K % 128 && tiles > 48 && tiles <= 256;
+    switch (t) {
+        // one round of blocks: a stage more in flight (6.9 against 7.8 us at N = K = 5120)
+        case Int8Tiles::FEW_16x32: return {t, !experts && rows <= 16 && tiles <= 256 ? 3 : 2, false};
+        case Int8Tiles::T64x32:
+        case Int8Tiles::T64x64: return {t, 4, false};
+        case Int8Tiles::T64x128: return {t, lines ? 4 : 3, lines};
+        case Int8Tiles::T128x128: return {t, tiles <= 256 ? 4 : 2, lines};                            // a block alone on its CU, or two
+        default: return {t, 2, false};
+    }
+}
+
 }  // namespace svdq
