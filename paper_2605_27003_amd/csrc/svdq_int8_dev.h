@@ -40,6 +40,11 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
     return v;
 }
 
+// An output from its exact sum: rounded to binary32, times the token's scale, then one multiplication and addition that round once, in every kernel alike.
+__device__ __forceinline__ float output(const int sum, const float sx, const float sw, const float bias) {
+    return __builtin_fmaf(__fmul_rn((float)sum, sx), sw, bias);
+}
+
 // Number of the first offset past a row, E + 1 if there is none: the row is the expert's before it (the running maximum of the offsets passes
 // the row where the first offset does).  Wave-uniform; all lanes take part.
 __device__ __forceinline__ int first_offset_past(const Groups& g, const int64_t row, const int lane) {

@@ -152,7 +152,7 @@ void gemm_int8_few_kernel(const GemmInt8 g, const int walkers) {
             int sum = 0;
 #pragma unroll
             for (int w = 0; w < NW; ++w) sum += (int)lds_read4(from + w * SUMS);
-            const float r = ((float)sum * bits_f(lds_read4(scales + m * 4))) * cs + cb;
+            const float r = output(sum, bits_f(lds_read4(scales + m * 4)), cs, cb);
             if (m < rows && n < cols) {
                 if constexpr (sizeof(T) == 2) y[(int64_t)m * g.ldy] = (T)f_bf16_rne(r);
                 else y[(int64_t)m * g.ldy] = f_bits(r);

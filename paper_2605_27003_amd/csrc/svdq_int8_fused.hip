@@ -178,7 +178,7 @@ void layer_int8_kernel(const QuantInt8 q, const GemmInt8 g) {
         int sum = 0;
 #pragma unroll
         for (int w = 0; w < NW; ++w) sum += (int)lds_read4(from + w * SUMS);
-        const float r = ((float)sum * bits_f(lds_read4(scales + m * 4))) * cs + cb;
+        const float r = output(sum, bits_f(lds_read4(scales + m * 4)), cs, cb);
         if (m < rows && n < cols) y[(int64_t)m * g.ldy] = (uint16_t)f_bf16_rne(r);
     }
 }

@@ -1,5 +1,5 @@
 // The product of the 8-bit layer on the int8 matrix cores: y = (qx qw^T) sx sw + bias, 32-bit integer sums over all of K (exact
-// for every K the interface takes: K 127^2 < 2^31), then three binary32 operations and one rounding to the output's type.
+// for every K the interface takes: K 128^2 < 2^31), then three binary32 roundings and one to the output's type (svdq_int8_dev.h, output).
 //
 // v_mfma_i32_16x16x64_i8: lane l holds row l % 16 of its operand and the 16 consecutive k [16 (l / 16), +16) as 16 bytes.  As in the
 // 4-bit kernels the transposed tile D[n][m] is computed (weights are the A operand), so that a lane owns token l % 16 and the four
@@ -52,7 +52,7 @@ struct TileStore {
                     for (int mi = 0; mi < MP; ++mi) {
                         float v[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) v[i] = ((float)acc[ni][m0 + mi][i] * ts[mi]) * s[i] + b[i];
+                        for (int i = 0; i < 4; ++i) v[i] = output(acc[ni][m0 + mi][i], ts[mi], s[i], b[i]);
                         const uint32_t to = region + (mi * I + li) * PITCH + (cb * I + at) * (int)sizeof(T);
                         if constexpr (sizeof(T) == 2) {
                             lds_write8_pinned(to, uint2{f2_bf16_rne(v[0], v[1]), f2_bf16_rne(v[2], v[3])});

@@ -33,3 +33,19 @@ def test_product_of_each_kernel(M, N, K, E):
             svdq.linear_w8a8(q, s, qw, sw, bias, out=y.t)
             check_product(y.t, q, s, qw, sw, bias)
         assert y.intact(owned)
+
+
+@pytest.mark.parametrize("N,K", [(515, 1040), (2048, 5120), (5120, 2048)])
+def test_a_row_is_the_same_bits_in_every_kernel(N, K):
+    """Alone, among a few and among thousands, dense and grouped: the sums are exact and what follows rounds alike, so a batch's size changes no row."""
+    M = 6000
+    g = torch.Generator("cuda").manual_seed(K)
+    q, qw = (torch.randint(-127, 128, shape, generator=g, device="cuda", dtype=I8) for shape in ((M, K), (N, K)))
+    s, sw, bias = 0.01 + torch.rand(M, generator=g, device="cuda"), 0.01 + torch.rand(N, generator=g, device="cuda"), 100.0 * torch.randn(N, generator=g, device="cuda")
+    for dtype, bits in ((BF16, torch.int16), (F32, torch.int32)):
+        want = svdq.linear_w8a8(q, s, qw, sw, bias, out_dtype=dtype).view(bits)
+        for m in (1, 9, 24, 40, 70, 130, 300, 600, 1100, 2305, 4000):
+            assert torch.equal(svdq.linear_w8a8(q[-m:], s[-m:], qw, sw, bias, out_dtype=dtype).view(bits), want[-m:]), m
+        for m in (5, 200, 3000):
+            got = svdq.linear_w8a8_grouped(q[:m], s[:m], offsets_of([m // 3, m - m // 3]), qw.expand(2, N, K).contiguous(), sw.expand(2, N).contiguous(), bias.expand(2, N).contiguous(), out_dtype=dtype)
+            assert torch.equal(got.view(bits), want[:m]), m
