@@ -316,6 +316,7 @@ void gemm_int8_kernel(const GemmInt8 g) {
     }
     stage(s, IC<0>{}, IC<1>{}, IC<1>{});
 
+    const int own_lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0)) & 63;      // no register through the K loop for it
     const uintptr_t ends = reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)(g.ldy * (int64_t)sizeof(T));
     const int unit = (ends & 15) == 0 ? 16 : (ends & 3) == 0 ? 4 : 2;
     const int mw = m0 + wm * MT * I, nw = n0 + wn * NT * I;
@@ -323,7 +324,7 @@ void gemm_int8_kernel(const GemmInt8 g) {
     const int below = (int)(scales - ring_a) / Store::BYTES;          // waves whose store area fits below the scales
     const uint32_t region = wave < below ? ring_a + wave * Store::BYTES : scales + G::SCALES + (wave - below) * Store::BYTES;
     Store::run(acc, region, scales + wm * MT * I * 4, scales + (G::TOKENS + wn * NT * I) * 4, scales + (G::TOKENS + G::CHANNELS + wn * NT * I) * 4,
-               at.bias != nullptr, lane, reinterpret_cast<T*>(g.y) + (int64_t)mw * g.ldy + nw, g.ldy, m_end - mw, N - nw, unit);
+               at.bias != nullptr, own_lane, reinterpret_cast<T*>(g.y) + (int64_t)mw * g.ldy + nw, g.ldy, m_end - mw, N - nw, unit);
 }
 
 template <class G>

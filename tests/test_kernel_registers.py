@@ -2,6 +2,7 @@
 import os
 import re
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 
 from paper_2605_27003_amd.build import CSRC, FLAGS, HIPCC
 
@@ -28,3 +29,10 @@ def test_few_token_kernels():
     assert not any(scratch.values()), scratch
     packed = [n for k, n in used.items() if "small_gemm_kernelILi1ELi1ELi1E" in k]
     assert len(packed) == 1 and packed[0] >= 84, packed
+
+
+def test_8_bit_kernels():
+    """None in scratch.  The 256 x 256 tiles have all 256 registers: one value more would go to memory and back in every tile."""
+    with ThreadPoolExecutor(4) as pool:
+        for used, scratch in pool.map(resources, ("svdq_int8_gemm.hip", "svdq_int8_few.hip", "svdq_int8_fused.hip", "svdq_int8_quant.hip")):
+            assert scratch and not any(scratch.values()), {k: v for k, v in scratch.items() if v}
