@@ -184,9 +184,7 @@ hipError_t launch(const GemmInt8& g, const bool out_f32, hipStream_t stream) {
 hipError_t launch_gemm_int8_few(const GemmInt8& g, const Int8Kernel& k, bool out_f32, hipStream_t stream) {
     switch (k.tiles) {
         case Int8Tiles::FEW_16x16: return launch<16, 16, 8, 2>(g, out_f32, stream);
-        case Int8Tiles::FEW_16x32:
-            if (k.depth == 3) return launch<16, 32, 4, 3>(g, out_f32, stream);
-            return launch<16, 32, 4, 2>(g, out_f32, stream);
+        case Int8Tiles::FEW_16x32: return launch<16, 32, 4, 2>(g, out_f32, stream);
         case Int8Tiles::FEW_32x16: return launch<32, 16, 8, 2>(g, out_f32, stream);
         default: return launch<32, 32, 4, 2>(g, out_f32, stream);
     }

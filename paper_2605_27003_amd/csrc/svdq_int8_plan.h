@@ -104,8 +104,6 @@ inline Int8Kernel int8_kernel(Int8Tiles t, int64_t rows, int N, int K, int exper
     // one tile of 128 x 128 takes up to 1.29 times as long, 48 to 256 tiles 0.7 to 1.1 times, 0.94 in the mean of 80 products.)
     const bool lines = K % 128 && tiles > 48 && tiles <= 256;
     switch (t) {
-        // one round of blocks: a stage more in flight (6.9 against 7.8 us at N = K = 5120)
-        case Int8Tiles::FEW_16x32: return {t, !experts && rows <= 16 && tiles <= 256 ? 3 : 2, false};
         case Int8Tiles::T64x32:
         case Int8Tiles::T64x64: return {t, 4, false};
         case Int8Tiles::T64x128: return {t, lines ? 4 : 3, lines};

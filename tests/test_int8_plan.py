@@ -101,4 +101,4 @@ def test_products_of_the_gpu_tests_reach_every_kernel(tmp_path):
     assert not wrong, wrong
     tested = {(*now, int(call[2] % 128 == 0), int(call[3] > 0), f32) for f32 in (0, 1) for (_, call), now in zip(calls, took[f32::2])}
     taken = set(ask())
-    assert len(taken) >= 100 and not taken - tested, taken - tested
+    assert len(taken) >= 90 and not taken - tested, taken - tested
