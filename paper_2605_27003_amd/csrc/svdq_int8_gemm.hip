@@ -327,7 +327,8 @@ void gemm_int8_kernel(const GemmInt8 g) {
                at.bias != nullptr, own_lane, reinterpret_cast<T*>(g.y) + (int64_t)mw * g.ldy + nw, g.ldy, m_end - mw, N - nw, unit);
 }
 
-template <class G>
+// WHOLE: of a K of whole stages only.
+template <class G, bool WHOLE = false>
 hipError_t launch_tiles(const GemmInt8& g, const bool out_f32, hipStream_t stream) {
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(most_tiles(g, G::BM, G::BN)), dim3(G::THREADS), 0, stream, g); };
     auto typed = [&](auto TAILC, auto GROUPEDC) {
@@ -336,8 +337,13 @@ hipError_t launch_tiles(const GemmInt8& g, const bool out_f32, hipStream_t strea
         else go(gemm_int8_kernel<G, TAIL, GROUPED, uint16_t>);
     };
     const bool grouped = g.groups.offsets != nullptr;
-    if (G::LINES || g.K % BK) grouped ? typed(IC<1>{}, IC<1>{}) : typed(IC<1>{}, IC<0>{});
-    else if constexpr (!G::LINES) grouped ? typed(IC<0>{}, IC<1>{}) : typed(IC<0>{}, IC<0>{});
+    if constexpr (!WHOLE) {
+        if (G::LINES || g.K % BK) {
+            grouped ? typed(IC<1>{}, IC<1>{}) : typed(IC<1>{}, IC<0>{});
+            return hipGetLastError();
+        }
+    }
+    if constexpr (!G::LINES) grouped ? typed(IC<0>{}, IC<1>{}) : typed(IC<0>{}, IC<0>{});
     return hipGetLastError();
 }
 
@@ -353,7 +359,7 @@ hipError_t launch_gemm_int8(const GemmInt8& g, const Int8Plan& p, bool out_f32, 
             return launch_tiles<Int8Tile<64, 128, 2, 4, 3>>(g, out_f32, stream);
         case Int8Tiles::T128x128:
             if (k.lines) return launch_tiles<Int8Tile<128, 128, 2, 4, 4, true>>(g, out_f32, stream);
-            if (k.depth == 4) return launch_tiles<Int8Tile<128, 128, 2, 4, 4>>(g, out_f32, stream);
+            if (k.depth == 4) return launch_tiles<Int8Tile<128, 128, 2, 4, 4>, true>(g, out_f32, stream);
             return launch_tiles<Int8Tile<128, 128, 2, 4, 2>>(g, out_f32, stream);
         case Int8Tiles::T256x128: return launch_tiles<Int8Tile<256, 128, 4, 2, 2>>(g, out_f32, stream);
         case Int8Tiles::T256x160: return launch_tiles<Int8Tile<256, 160, 4, 2, 2>>(g, out_f32, stream);

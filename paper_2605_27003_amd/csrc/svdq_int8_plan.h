@@ -107,7 +107,8 @@ inline Int8Kernel int8_kernel(Int8Tiles t, int64_t rows, int N, int K, int exper
         case Int8Tiles::T64x32:
         case Int8Tiles::T64x64: return {t, 4, false};
         case Int8Tiles::T64x128: return {t, lines ? 4 : 3, lines};
-        case Int8Tiles::T128x128: return {t, tiles <= 256 ? 4 : 2, lines};                            // a block alone on its CU, or two
+        // a block alone on its CU, or two.  (Up to 48 tiles the estimate takes smaller ones.)
+        case Int8Tiles::T128x128: return {t, tiles <= 256 && (lines || K % 128 == 0) ? 4 : 2, lines};
         default: return {t, 2, false};
     }
 }
