@@ -75,3 +75,28 @@ def test_runs_of_as_many_rows_as_there_are():
     rows = torch.randperm(M, device="cuda").to(I32)
     offsets = offsets_of(loads_of(1, M, E))
     check_quantised(*svdq.quantize_act_int8_grouped(x, offsets, il, rho, rows=rows), *quantise64(x[rows.long()], il[experts_of(offsets, M)], rho))
+
+
+@pytest.mark.parametrize("M,N,K,E,gelu", [(5003, 1300, 5120, 0, False), (26300, 640, 5120, 0, True), (17001, 515, 1552, 0, True), (9001, 1300, 5120, 2, False), (9001, 648, 4112, 3, True),
+                                          (5003, 768, 2048, 128, False), (4999, 515, 13824, 2, True)])
+def test_layers_of_many_rows_are_their_two_halves(M, N, K, E, gelu):
+    """Bit for bit, with rows given in another order where the layer is grouped; and x as its own output where its rows are as long."""
+    g = torch.Generator("cuda").manual_seed(M + K)
+    lead = (E,) if E else ()
+    qw = torch.randint(-127, 128, (*lead, N, K), generator=g, device="cuda", dtype=I8)
+    sw, bias = 0.001 * torch.rand((*lead, N), generator=g, device="cuda"), torch.randn((*lead, N), generator=g, device="cuda")
+    il, x = 0.5 + torch.rand((*lead, K), generator=g, device="cuda"), activations(K, M, K)
+    if E:
+        rho, rows, offsets = 0.3 + 0.7 * torch.rand(M, generator=g, device="cuda"), torch.randperm(M, generator=g, device="cuda").to(I32), offsets_of(loads_of(M, M, E))
+        layer = svdq.W8A8Experts(il, qw, sw, bias)
+        qx, sx = svdq.quantize_act_int8_grouped(x, offsets, il, rho, rows=rows, gelu=gelu)
+        want, call = svdq.linear_w8a8_grouped(qx, sx, offsets, qw, sw, bias), lambda **kw: layer.forward(x, offsets, rho, rows=rows, gelu=gelu, **kw)
+    else:
+        layer = svdq.W8A8Linear(il, qw, sw, bias)
+        qx, sx = svdq.quantize_act_int8(x, il, 0.9, gelu=gelu)
+        want, call = svdq.linear_w8a8(qx, sx, qw, sw, bias), lambda **kw: layer.forward(x, 0.9, gelu=gelu, **kw)
+    y = Guarded(M, N, BF16, ld=N + 8)
+    assert torch.equal(call().view(torch.int16), want.view(torch.int16))
+    call(out=y.t)
+    assert torch.equal(y.t.contiguous().view(torch.int16), want.view(torch.int16)) and y.intact()
+    assert torch.equal(call(out=x[:, :N]).contiguous().view(torch.int16), want.view(torch.int16))
