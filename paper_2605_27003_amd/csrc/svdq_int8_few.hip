@@ -6,6 +6,9 @@
 // registers.  (Operands straight to registers would be sixteen rows' pieces a load: 38 bytes a ns a CU from L2 where transfers of
 // whole lines, eight lanes a row, reach 135.)  Blocks walk the tiles: a wave's requests run on into its next tiles while sums are added up and
 // stored, since with a short K a tile is little more than its start.  The partial sums, exact integers in any order, meet in LDS.
+//
+// Times here are of calls that find their weights in the 256 MB memory-side cache, left there by the call before.  Where every call has weights of its
+// own, as the layers of a model have: 157 MB for one token 28.1 us for 23.2 (5.6 TB/s), 26 MB for 24 tokens 10.1 for 6.8, replayed from a graph.
 #include "svdq_int8_dev.h"
 #include "svdq_int8_plan.h"
 

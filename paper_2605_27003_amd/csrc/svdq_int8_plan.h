@@ -42,7 +42,9 @@ struct Int8Plan {
 //   memory     weights and codes at 5.5 TB/s, outputs at 4.4 where their rows are whole memory lines and at 3.3 where tiles share lines (8318 x 28896 of
 //              binary32 at K = 176: 240 us; 28884 channels: 436)
 // and a little of each, which decides where choices share their bound.  A tile that has its CU alone has nothing to overlap its stores with.
-// The figures are fitted to 900 calls of 1 to 75600 rows, each timed with every tile: the choice is 1.8 % slower than the best in the mean, a third at worst.
+// The figures are fitted to 900 calls of 1 to 75600 rows, each timed with every tile (beyond 4000 rows with those of 64 rows and more), before there were kernels that
+// fetch whole lines, which the estimate does not know.  On the calls that it was fitted to the choice is 1.9 % slower than the best tile timed in the mean,
+// a third at worst; six of them, more than 5000 rows by 10 to 25 channels, take few-token tiles, which were not timed there.
 inline Int8Plan int8_cost(Int8Tiles t, int64_t rows, int N, int K, int experts, bool out_f32) {
     const Int8TileShape s = int8_tile_shape(t);
     const int64_t with_rows = experts ? (rows < experts ? rows : experts) : 1, nt = ((int64_t)N + s.bn - 1) / s.bn;

@@ -1,8 +1,8 @@
 // Activations of the 8-bit layer: one pass over x that smooths (eq. 5), finds every token's largest magnitude, derives its clipped
 // scale s = (rho a) / 127 (eq. 8-9) and rounds its codes (eq. 3), K + 4 bytes written for 2 K read.
 //
-// A token's scale needs the whole row, so the row stays in registers between the maximum and the rounding: a wave, four or
-// sixteen of them share a row, eight consecutive k a lane and chunk.  The block walks a run of rows with the smoothing vector in
+// A token's scale needs the whole row, so the row stays in registers between the maximum and the rounding: a wave, two, four
+// or sixteen of them share a row, eight consecutive k a lane and chunk.  The block walks a run of rows with the smoothing vector in
 // registers (it is twice a row's bytes) and the next row's x under way; one barrier a row where waves share it, on
 // two alternating sets of partial maxima.
 //
@@ -152,9 +152,12 @@ void quantize_int8_kernel(const QuantInt8 q, const int run) {
 template <int W, int C>
 hipError_t launch_rows(const QuantInt8& q, const bool gelu, hipStream_t stream) {
     constexpr int TEAMS = W <= 4 ? 4 / W : 1, THREADS = W <= 4 ? 256 : 64 * W;
-    // Eight blocks a CU, which are there at once, then longer runs of rows (at most 64: a lane holds each row's token and ratio; rounded up, since a few blocks
-    // more wait for a place: grouped 25786 x 2832 in 1075 blocks of a place for 1024 50.6 us, in 992 39.3).  Grouped, a block begins with its expert, token and
-    // smoothing vector one after the other: with few rows an expert four (128 rows each of K = 2048: 17.3 us, with eight 19.3; 16380 of K = 5120: 113.7 and 105.2).
+    // Up to 2048 blocks, eight a CU, then longer runs of rows, of 16 at most (a lane holds each row's token and ratio); beyond those, more blocks.  Eight
+    // are there at once where a lane has one chunk or two.  The registers of three leave room for five, of four for four, of five (32760 x 5120) for three and
+    // of seven for two, and sixteen waves have a CU to themselves: there blocks wait for a place.  Rounded up, since a few blocks more than places are a
+    // round more (grouped 25786 x 2832 in 1075 blocks of a place for 1024 50.6 us, in 992 39.3).  Grouped, a block begins with its expert, token and
+    // smoothing vector one after the other: with few rows an expert 1024 blocks (128 rows each of K = 2048: 17.3 us, with 2048 19.3; 16380 of K = 5120: 113.7
+    // and 105.2).
     const bool four = q.groups.offsets && q.M / q.groups.E < 1024;
     const int64_t teams = (int64_t)TEAMS * (four ? 1024 : 2048);
     int64_t run = (q.M + teams - 1) / teams;
