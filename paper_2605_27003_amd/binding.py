@@ -95,10 +95,9 @@ def _ptr(t):
 # hipStream_t of the current stream of the current device.  torch.cuda.current_stream() builds a Stream object for it:
 # 2.8 us against 0.1 us, of the 12 us that the host needs for a layer with few tokens.  Where torch has renamed its own
 # functions, the public way.
-def _raw_stream(current=None):
-    """current: the current device, where the caller knows it."""
+def _raw_stream():
     try:
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice() if current is None else current)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     except AttributeError:
         return torch.cuda.current_stream().cuda_stream
 
@@ -686,16 +685,15 @@ class W4A4Linear:
 # ---- the 8-bit layer, and its form grouped by expert ---------------------------------------------
 # Arguments are checked here for what the C functions cannot see (types, shapes, devices): a few comparisons a tensor, words only
 # where one fails, since calls with few tokens wait for the host.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", lambda gpu: torch.cuda.current_stream(gpu).cuda_stream)
+
+
 def _gpu(t):
     """The GPU that holds t, which has to be the current one."""
     gpu = t.get_device()
-    if gpu >= 0:
-        try:
-            current = torch._C._cuda_getDevice()
-        except AttributeError:
-            current = torch.cuda.current_device()
-        if gpu == current:
-            return gpu
+    if gpu >= 0 and gpu == _current_device():
+        return gpu
     raise ValueError(f"tensors on the current GPU are needed, not on {t.device}")
 
 
@@ -752,7 +750,7 @@ def quantize_act_int8(x_bf16, inv_lambda=None, rho=1.0, gelu=False, out=None):
     qx, sx = _quantize_int8_out(out, M, K, x_bf16, gpu)
     if M:                            # an empty tensor has no address
         _check((_lib or load_library()).svdq_quantize_act_int8(x_bf16.data_ptr(), ldx, il, float(rho), 1 if gelu else 0, M, K, qx.data_ptr(), sx.data_ptr(),
-                                                               _raw_stream(gpu)), "svdq_quantize_act_int8")
+                                                               _stream_of(gpu)), "svdq_quantize_act_int8")
     return qx, sx
 
 
@@ -778,7 +776,7 @@ def linear_w8a8(qx, sx, qw, sw, bias=None, out=None, out_dtype=torch.bfloat16):
     pb = None if bias is None else _vector("bias", bias, _F32, N, gpu)
     y, ldy, code = _linear_out(out, M, N, out_dtype, qx, gpu)
     if M:
-        _check((_lib or load_library()).svdq_linear_w8a8(pq, ps, pw, pc, pb, M, N, K, y.data_ptr(), ldy, code, _raw_stream(gpu)), "svdq_linear_w8a8")
+        _check((_lib or load_library()).svdq_linear_w8a8(pq, ps, pw, pc, pb, M, N, K, y.data_ptr(), ldy, code, _stream_of(gpu)), "svdq_linear_w8a8")
     return y
 
 
@@ -802,7 +800,7 @@ def quantize_act_int8_grouped(x_bf16, offsets, inv_lambda=None, rho=1.0, rows=No
     qx, sx = _quantize_int8_out(out, M, K, x_bf16, gpu)
     if M:
         _check((_lib or load_library()).svdq_quantize_act_int8_grouped(
-            x_bf16.data_ptr(), ldx, x_rows, r, o, E, il, ratio, row_rho, 1 if gelu else 0, M, K, qx.data_ptr(), sx.data_ptr(), _raw_stream(gpu)),
+            x_bf16.data_ptr(), ldx, x_rows, r, o, E, il, ratio, row_rho, 1 if gelu else 0, M, K, qx.data_ptr(), sx.data_ptr(), _stream_of(gpu)),
             "svdq_quantize_act_int8_grouped")
     return qx, sx
 
@@ -819,7 +817,7 @@ def linear_w8a8_grouped(qx, sx, offsets, qw, sw, bias=None, out=None, out_dtype=
     o = _vector("offsets", offsets, _I32, E + 1, gpu)
     y, ldy, code = _linear_out(out, M, N, out_dtype, qx, gpu)
     if M:
-        _check((_lib or load_library()).svdq_linear_w8a8_grouped(pq, ps, pw, pc, pb, o, E, M, N, K, y.data_ptr(), ldy, code, _raw_stream(gpu)), "svdq_linear_w8a8_grouped")
+        _check((_lib or load_library()).svdq_linear_w8a8_grouped(pq, ps, pw, pc, pb, o, E, M, N, K, y.data_ptr(), ldy, code, _stream_of(gpu)), "svdq_linear_w8a8_grouped")
     return y
 
 
@@ -889,7 +887,7 @@ class _W8A8:
                 scales = codes + M * K
             rc = (_lib or load_library()).svdq_layer_int8_forward(
                 layer.address, x.data_ptr(), ldx, x_rows, rows, offsets, rho, row_rho, 1 if gelu else 0, M,
-                codes, scales, y.data_ptr(), ldy, _raw_stream(gpu))
+                codes, scales, y.data_ptr(), ldy, _stream_of(gpu))
             if rc:
                 _check(rc, "svdq_layer_int8_forward")
         return y
